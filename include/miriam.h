@@ -264,6 +264,99 @@ int miriam_op_reset_counters(const miriam_op *op, void *stream);
 /* Release the operator.  MIRIAM_EBUSY if a submitted task that uses it is pending. */
 int miriam_op_destroy(miriam_op *op);
 
+/* ------------------------------------------- operators over packed token rows
+ *
+ * What lies between the matrix products of a decoder layer, as elastic operators: they are launched,
+ * queried, sharded, grouped into tasks and destroyed like the others.
+ *
+ * A batch is `seqs` sequences whose new tokens lie packed in `tokens` rows (a capacity): sequence s has rows
+ * q_start[s] .. q_start[s + 1] - 1, and kv_len[s] keys once its new tokens are in the cache, so its i-th new
+ * token is at position kv_len[s] - (q_start[s + 1] - q_start[s]) + i.  The cache holds `pages` pages of `page`
+ * tokens for `kv_heads` heads; row s of the page table names the pages of sequence s in order.  These three
+ * arrays are read on the device by every pass, so one operator (and one captured graph of it) serves batches
+ * of any lengths within its capacities.  They are clamped there, so that no value of theirs leads outside the
+ * buffers: starts to 0 .. tokens, lengths to 0 .. max_pages * page; a page outside 0 .. pages - 1 is absent:
+ * its keys are not there for any query and nothing is stored to it.  Rows that belong to no sequence are left
+ * as they were.
+ *
+ * The coordinator runs an operator several times when it measures it, so none of these works in place: an
+ * output that overlaps an input is refused (columns of their own in rows of one buffer are no overlap).
+ */
+typedef enum {
+    /* Norms around a block, with its gate and residual, over rows of n values:
+     *   u = N(x; post, post_bias) (x itself without post);  u = gate(u);  h = residual + scale * u;
+     *   y = h;  z = N(h; pre, pre_bias), h as it is before its rounding to y.
+     * N is RMS norm, v / sqrt(mean(v^2) + eps) * weight (+ bias), or layer norm (MIRIAM_SEQ_LAYER_NORM),
+     * which subtracts the mean first.  residual, post, gate, the biases and either of y and z (with pre) may
+     * be absent.  Sums are held in fp32. */
+    MIRIAM_OP_BLOCK_NORM = 16,
+    /* Rotary positions and the append to the cache.  x holds (heads + 2 kv_heads) heads of head_dim per row:
+     * queries, keys, values.  Of the queries and keys the first `rot` values are turned pairwise by position *
+     * freq[j]: (a, b) -> scale * (a cos - b sin, b cos + a sin), the pairs being (j, j + rot / 2), or (2 j,
+     * 2 j + 1) with MIRIAM_SEQ_INTERLEAVED; the others are copied.  Queries go to y (heads heads per row), keys
+     * and values to the token's place in the cache.  Angles are reduced in 64 bits, so far positions lose
+     * nothing.  kv_heads = 0: no cache, every head goes to y.  A token at a negative position is turned, not
+     * stored.  Two new tokens must not share a place in the cache. */
+    MIRIAM_OP_ROTARY = 17,
+    /* Attention of the new tokens over the paged cache: y = sum_j softmax_j(scale * q . k_j) v_j for every
+     * query head, heads / kv_heads consecutive ones sharing a cache head, over the keys j < kv_len[s] that
+     * are there and, with MIRIAM_SEQ_CAUSAL, at or before the token's position, and with window > 0 among the
+     * `window` last ones up to it.  A row without keys gives zeros, and what a row does not see never reaches
+     * it, whatever it holds (infinities and NaN included).  fp16 / bf16.  max_q: most new tokens of one
+     * sequence (0 = tokens); rows of a sequence behind its max_q-th are left as they were.  A query's keys may
+     * be divided among tiles, whose partial results the last one to finish joins in a fixed order: such an op
+     * (miriam_op_info.ksplit > 1) owns a device workspace and arrival counters, with the rules of split K:
+     * every pass covers the whole tile space, passes over one op do not overlap in time. */
+    MIRIAM_OP_ATTENTION = 18
+} miriam_seq_kind;
+
+enum {
+    MIRIAM_SEQ_INTERLEAVED = 1, /* ROTARY: pairs (2 j, 2 j + 1) */
+    MIRIAM_SEQ_CAUSAL = 2,      /* ATTENTION: no key after the token's own position */
+    MIRIAM_SEQ_LAYER_NORM = 4   /* BLOCK_NORM: layer norm (RMS norm without) */
+};
+
+typedef enum {
+    MIRIAM_GATE_NONE = 0,
+    MIRIAM_GATE_CHANNEL = 1, /* u * gate[c], float32[n] */
+    MIRIAM_GATE_ROWS = 2,    /* u * gate, rows of the operator's dtype */
+    MIRIAM_GATE_SILU = 3,    /* u * gate / (1 + exp(-gate)), rows */
+    MIRIAM_GATE_SIGMOID = 4  /* u / (1 + exp(-gate)), rows */
+} miriam_gate;
+
+/* Fields not used by a kind are ignored.  Row strides (ld*) and the cache strides are in elements; a row
+ * stride of 0 means dense rows, page_table's is ldt (0 = max_pages). */
+typedef struct miriam_seq_desc {
+    int32_t kind;     /* miriam_seq_kind */
+    int32_t dtype;    /* miriam_dtype of x, y, z, residual, row gates and the caches */
+    int32_t flags;    /* MIRIAM_SEQ_* */
+    int32_t gate_kind; /* BLOCK_NORM: miriam_gate */
+    int64_t tokens;   /* rows */
+    int64_t n;        /* BLOCK_NORM: values per row */
+    int64_t seqs, heads, kv_heads, head_dim;
+    int64_t rot;      /* ROTARY: turned values of a head, even, at most head_dim */
+    int64_t max_q, window; /* ATTENTION */
+    int64_t page, pages, max_pages;
+    int64_t ldx, ldy, ldz, ldr, ldg, ldt;
+    int64_t cache_page, cache_head, cache_token; /* strides of both caches, elements */
+    float scale;      /* BLOCK_NORM: of the block; ROTARY: of the turned values; ATTENTION: of q . k */
+    float eps;        /* BLOCK_NORM */
+    const void *x;
+    void *y, *z;
+    const void *residual, *gate;
+    const float *post, *post_bias, *pre, *pre_bias;  /* float32[n] */
+    const int32_t *q_start, *kv_len, *page_table;    /* device: [seqs + 1], [seqs], [seqs][ldt] */
+    void *k_cache, *v_cache;
+    const double *freq; /* ROTARY: device, rot / 2 angles per position, radians */
+} miriam_seq_desc;
+
+/* Validate *d and create an operator that borrows its device pointers until miriam_op_destroy.  Errors as
+ * miriam_op_create; launches are refused (MIRIAM_EINVAL) while another device than that of the creation is
+ * current.  The _noalloc form takes an attention workspace from the device scratch of
+ * miriam_op_create_noalloc, under its rules, dividing less where that is too small. */
+int miriam_seq_op_create(const miriam_seq_desc *d, miriam_op **out);
+int miriam_seq_op_create_noalloc(const miriam_seq_desc *d, miriam_op **out);
+
 /* ------------------------------------------------------ planning (host only) */
 
 /* Eq. (1): dichotomy slice widths of a kernel with M blocks, smallest first.
@@ -297,6 +390,13 @@ int miriam_plan_top_fraction(int n, const double *score, const int64_t *grid,
 /* §7 shaded binary tree: length of the shallowest node that starts at `cursor` and
  * holds at most max_len tiles; *depth receives its depth.  Negative on bad input. */
 int64_t miriam_plan_tree_head(int64_t T, int64_t cursor, int64_t max_len, int *depth);
+
+/* Angles per position for ROTARY, radians: f_j = base^(-2 j / rot), j < rot / 2, for a context stretched by
+ * `factor` >= 1.  original > 0: by parts, f_j where it makes `high` turns or more over the original context,
+ * f_j / factor where it makes `low` or fewer, and in between their mean by the turns' place in that interval
+ * (0 <= low < high); original = 0: every f_j / factor.  Host memory. */
+int miriam_plan_rotary_freqs(int64_t rot, double base, double factor, int64_t original, double low, double high,
+                             double *freq);
 
 /* ------------------------------------------------------------- coordinator */
 

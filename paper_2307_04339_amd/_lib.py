@@ -24,6 +24,9 @@ ACT_NONE, ACT_RELU, ACT_RELU6, ACT_GELU = 0, 1, 2, 3
 ACT_CODE = {"none": 0, "relu": 1, "relu6": 2, "gelu": 3}
 EPI_BIAS, EPI_BN, EPI_RESIDUAL = 1, 2, 4
 INDEX_MEMORY = 8  # memory-based index function (host-computed row table)
+OP_BLOCK_NORM, OP_ROTARY, OP_ATTENTION = 16, 17, 18
+SEQ_INTERLEAVED, SEQ_CAUSAL, SEQ_LAYER_NORM = 1, 2, 4
+GATE_NONE, GATE_CHANNEL, GATE_ROWS, GATE_SILU, GATE_SIGMOID = range(5)
 POLICY_ELASTIC, POLICY_SEQUENTIAL, POLICY_MULTISTREAM, POLICY_IB = 0, 1, 2, 3
 BACKEND_HIP, BACKEND_FAKE = 0, 1
 
@@ -45,6 +48,25 @@ class OpDesc(ctypes.Structure):
         ("eps", ctypes.c_float), ("scale", ctypes.c_float),
         ("x", ctypes.c_void_p), ("wt", ctypes.c_void_p), ("bias", ctypes.c_void_p),
         ("bn", ctypes.c_void_p), ("residual", ctypes.c_void_p), ("y", ctypes.c_void_p),
+    ]
+
+
+class SeqDesc(ctypes.Structure):
+    _fields_ = [
+        ("kind", ctypes.c_int32), ("dtype", ctypes.c_int32), ("flags", ctypes.c_int32),
+        ("gate_kind", ctypes.c_int32), ("tokens", ctypes.c_int64), ("n", ctypes.c_int64),
+        ("seqs", ctypes.c_int64), ("heads", ctypes.c_int64), ("kv_heads", ctypes.c_int64),
+        ("head_dim", ctypes.c_int64), ("rot", ctypes.c_int64), ("max_q", ctypes.c_int64),
+        ("window", ctypes.c_int64), ("page", ctypes.c_int64), ("pages", ctypes.c_int64),
+        ("max_pages", ctypes.c_int64), ("ldx", ctypes.c_int64), ("ldy", ctypes.c_int64),
+        ("ldz", ctypes.c_int64), ("ldr", ctypes.c_int64), ("ldg", ctypes.c_int64), ("ldt", ctypes.c_int64),
+        ("cache_page", ctypes.c_int64), ("cache_head", ctypes.c_int64), ("cache_token", ctypes.c_int64),
+        ("scale", ctypes.c_float), ("eps", ctypes.c_float),
+        ("x", ctypes.c_void_p), ("y", ctypes.c_void_p), ("z", ctypes.c_void_p),
+        ("residual", ctypes.c_void_p), ("gate", ctypes.c_void_p), ("post", ctypes.c_void_p),
+        ("post_bias", ctypes.c_void_p), ("pre", ctypes.c_void_p), ("pre_bias", ctypes.c_void_p),
+        ("q_start", ctypes.c_void_p), ("kv_len", ctypes.c_void_p), ("page_table", ctypes.c_void_p),
+        ("k_cache", ctypes.c_void_p), ("v_cache", ctypes.c_void_p), ("freq", ctypes.c_void_p),
     ]
 
 
@@ -136,6 +158,10 @@ SIGNATURES = {
     "miriam_elastic_launch_traced": ([_P, _I64, _I64, _INT, _INT, _P, _P, _P, _P, _P, _P], _INT),
     "miriam_op_destroy": ([_P], _INT),
     "miriam_op_reset_counters": ([_P, _P], _INT),
+    "miriam_seq_op_create": ([ctypes.POINTER(SeqDesc), ctypes.POINTER(_P)], _INT),
+    "miriam_seq_op_create_noalloc": ([ctypes.POINTER(SeqDesc), ctypes.POINTER(_P)], _INT),
+    "miriam_plan_rotary_freqs": ([_I64, ctypes.c_double, ctypes.c_double, _I64, ctypes.c_double, ctypes.c_double,
+                                  _DP], _INT),
     "miriam_plan_dichotomy": ([_I64, _I64P, _INT], _INT),
     "miriam_plan_split": ([_I64, _I64, _I64P, _I64P], _INT),
     "miriam_plan_wg_rank": ([_I64, _I64, _I64], _I64),

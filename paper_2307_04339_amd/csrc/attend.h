@@ -1,0 +1,106 @@
+// Attention over a paged cache: what its two kernels share.
+//
+//   o = sum_j p_j v_j / sum_j p_j,  p_j = 2^(c q . k_j - m),  c = scale * log2(e),  m the running maximum
+//
+// in one pass over the keys: when the maximum rises from m to m', the sums so far are multiplied by 2^(m - m').
+// Scores, maxima and sums are fp32.  Products run on the matrix cores with the keys as their rows, S^T = K Q^T
+// and O^T = V^T P^T, so that a lane owns one query row: its maximum, its sum and its factor need no broadcast,
+// and the scores leave the first product in the layout in which the second takes them, if the contraction
+// index over the keys is numbered accordingly (it may be, as any order of the keys gives the same sum).
+//
+// fp16: P is 2^kShift times larger than a probability relative to the maximum (the sum as well, so it cancels):
+// values down to 2^-24 of the largest are then normal fp16 numbers.
+#pragma once
+
+#include "igemm.h"
+#include "seq_rows.h"
+
+namespace miriam {
+
+template <class T> constexpr float kShift = 0.0f;
+template <> inline constexpr float kShift<half_t> = 10.0f;
+
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef __attribute__((address_space(3))) s16x4 *lds_s16x4;
+
+// 16 bytes of zeros: where keys that are not there are read.
+static __device__ __attribute__((aligned(64))) uint32_t g_no_key[16];
+
+// New tokens and keys of a sequence, for an op's batch.
+struct SeqView {
+    int q0, n;       // first packed row, rows (at most max_q)
+    int pos0;        // position of the first
+    int len;         // keys
+    int begin, end;  // keys that any of the rows may see
+};
+__device__ __forceinline__ SeqView seq_view(const AttendArgs &a, int64_t s) {
+    SeqView v;
+    v.q0 = clampi(a.sq.q_start[s], 0, (int)a.sq.tokens);
+    const int full = clampi(a.sq.q_start[s + 1], v.q0, (int)a.sq.tokens) - v.q0;
+    v.len = seq_len(a.sq, s);
+    v.pos0 = v.len - full;
+    v.n = full < a.max_q ? full : a.max_q;
+    v.end = a.causal ? clampi(v.pos0 + v.n, 0, v.len) : v.len;
+    v.begin = a.window > 0 ? clampi(v.pos0 - a.window + 1, 0, v.end) : 0;
+    return v;
+}
+
+// Element offset of key j (without the head's), -1 where there is none.
+__device__ __forceinline__ int64_t key_place(const AttendArgs &a, int64_t s, const SeqView &v, int j) {
+    return j >= v.begin && j < v.end ? cache_place(a.sq, (int)s, j) : -1;
+}
+
+__device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// Two 32-bit floats rounded to T, packed.
+template <class T>
+__device__ __forceinline__ uint32_t pack2(float a, float b) {
+    typedef T t2 __attribute__((ext_vector_type(2)));
+    typedef float f2 __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector((f2{a, b}), t2));
+}
+template <class T>
+__device__ __forceinline__ float unpack(uint32_t w, int hi) {
+    return TypeOps<T>::to_f(__builtin_bit_cast(T, (uint16_t)(hi ? w >> 16 : w & 0xffffu)));
+}
+
+// Whether any of the eight 16-bit values is an infinity or a NaN.
+template <class T>
+__device__ __forceinline__ bool not_finite(const u32x4 &v) {
+    constexpr uint32_t M = sizeof(T) == 2 && __is_same(T, half_t) ? 0x7c00u : 0x7f80u;
+    bool r = false;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) r |= ((v[i] & M) == M) | ((v[i] >> 16 & M) == M);
+    return r;
+}
+
+// Bits of the keys kb .. kb + 63 that the row at `pos` sees.
+__device__ __forceinline__ uint64_t seen_keys(const AttendArgs &a, int kb, int pos) {
+    auto upto = [](int n) -> uint64_t { return n >= 63 ? ~0ull : n < 0 ? 0ull : (2ull << n) - 1; };  // bits 0 .. n
+    uint64_t w = ~0ull;
+    if (a.causal) w = upto(pos - kb);
+    if (a.window > 0) w &= ~upto(pos - a.window - kb);
+    return w;
+}
+
+// Values of keys that some of the rows do not see.  Their probability is 0 for those rows, but 0 times an
+// infinity or a NaN is no 0: such values are added to the outputs of the rows that see them by themselves (no
+// probability but 0 makes another of them), and taken out of the product.
+template <class T>
+__device__ __forceinline__ u32x4 only_finite(u32x4 v) {
+    constexpr uint32_t M = __is_same(T, half_t) ? 0x7c00u : 0x7f80u;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] &= ((v[i] & M) == M ? 0u : 0xffffu) | ((v[i] >> 16 & M) == M ? 0u : 0xffff0000u);
+    return v;
+}
+template <class T>
+__device__ __forceinline__ float not_finite_of(uint32_t w, int hi, bool seen) {
+    constexpr uint32_t M = __is_same(T, half_t) ? 0x7c00u : 0x7f80u;
+    return seen && ((hi ? w >> 16 : w) & M) == M ? unpack<T>(w, hi) : 0.0f;
+}
+
+// Cache policy of a buffer access with agent-scope coherence.
+constexpr int kAgent = 16;
+
+}  // namespace miriam

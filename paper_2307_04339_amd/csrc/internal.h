@@ -9,13 +9,14 @@
 
 #include "../../include/miriam.h"
 #include "kargs.h"
+#include "seq_args.h"
 
 namespace miriam {
 
 void set_error(const std::string &msg);
 int hip_fail(hipError_t e, const char *what);  // records the HIP error text, returns MIRIAM_EHIP
 
-enum Family { FAM_IGEMM = 0, FAM_PIX = 1, FAM_ROW = 2, FAM_SKINNY = 3 };
+enum Family { FAM_IGEMM = 0, FAM_PIX = 1, FAM_ROW = 2, FAM_SKINNY = 3, FAM_NORM = 4, FAM_ROTARY = 5, FAM_ATTEND = 6 };
 
 // Kernel tables (one entry per physical block of 64, 128, 256 threads).
 int igemm_kernels_f32(int cfg, int lay, const void *out[3], int *lds);
@@ -42,6 +43,13 @@ int skinny_kernels(int dtype, int cg, const void *out[3]);  // cg: 16-column gro
 int skinny_group(int cg);                                   // K per wave group of that kernel
 // resident-weight direct convolution: (3x3, stride 1, C in {8,16,32,64}), (3x3, stride 2, C = 8),
 // (1x1, stride 1, C in {16,24,32,64})
+int norm_kernels(int dtype, int form, bool vec, const void *out[3]);  // form: NormForm
+int rotary_kernels(int dtype, bool vec, const void *out[3]);
+// attention, head_dim <= dp in {64, 128, 256}: up to 16 query rows per cache head, or tiles of 128
+int attend_rows_kernels_f16(int dp, const void *out[3], int *lds);
+int attend_rows_kernels_bf16(int dp, const void *out[3], int *lds);
+int attend_tile_kernels_f16(int dp, const void *out[3], int *lds);
+int attend_tile_kernels_bf16(int dp, const void *out[3], int *lds);
 int rw_kernels(int dtype, int64_t ks, int64_t stride, int64_t c, const void *out[3], int *lds);
 
 }  // namespace miriam
@@ -60,6 +68,11 @@ struct miriam_op {
     miriam::IgemmArgs ig;
     miriam::PixArgs px;
     miriam::RowArgs rw;
+    miriam_seq_desc sd;     // operators over packed token rows (families NORM, ROTARY, ATTEND)
+    int device = -1;        // and the device that they were created on
+    miriam::NormArgs nm;
+    miriam::RotaryArgs ro;
+    miriam::AttendArgs at;
     std::atomic<int> pending{0};  // submitted requests that still reference the op
     void *work = nullptr;         // split-K partial tiles (device memory owned by the op)
     void *counters = nullptr;     // split-K arrival counters (device memory owned by the op)

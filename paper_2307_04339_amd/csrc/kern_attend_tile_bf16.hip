@@ -1,0 +1,13 @@
+// Attention for tiles of query rows, bf16.
+#include "attend_tile.h"
+
+namespace miriam {
+int attend_tile_kernels_bf16(int dp, const void *out[3], int *lds) {
+    switch (dp) {
+    case 64: tile_table<bf16_t, 64>(out, lds); return 0;
+    case 128: tile_table<bf16_t, 128>(out, lds); return 0;
+    case 256: tile_table<bf16_t, 256>(out, lds); return 0;
+    default: return -1;
+    }
+}
+}  // namespace miriam

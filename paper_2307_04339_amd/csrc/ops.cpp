@@ -3,6 +3,7 @@
 // entry points (§6.1 elastic block, §6.2 elastic grid, §6.4 computation-based
 // index functions).
 #include <algorithm>
+#include <cmath>
 #include <cstdio>
 #include <cstring>
 #include <mutex>
@@ -829,6 +830,12 @@ static int create_row(miriam_op *op) {
     return MIRIAM_OK;
 }
 
+}  // namespace miriam
+
+#include "seq_create.h"
+
+namespace miriam {
+
 int op_launch(const miriam_op *op, int64_t b, int64_t l, int grid, int block, hipStream_t st,
               int32_t *owner_wg, int32_t *owner_iter, int32_t *count, int32_t *wave_phys, int32_t *wave_slot) {
     if (!op) return einval("null op");
@@ -853,6 +860,17 @@ int op_launch(const miriam_op *op, int64_t b, int64_t l, int grid, int block, hi
     case FAM_IGEMM:
     case FAM_SKINNY: args[0] = const_cast<IgemmArgs *>(&op->ig); break;
     case FAM_PIX: args[0] = const_cast<PixArgs *>(&op->px); break;
+    case FAM_NORM:
+    case FAM_ROTARY:
+    case FAM_ATTEND: {
+        int dev = -1;
+        if (hipGetDevice(&dev) != hipSuccess || dev != op->device) {
+            (void)hipGetLastError();
+            return einval("the op was created on another device than the current one");
+        }
+        args[0] = seq_args(op);
+        break;
+    }
     default: args[0] = const_cast<RowArgs *>(&op->rw); break;
     }
     args[1] = &sh;
@@ -871,6 +889,21 @@ int op_param_ranges(const miriam_op *op, const void *ptr[3], int64_t bytes[3]) {
     const miriam_op_desc &d = op->d;
     const int64_t es = esize(d.dtype);
     int n = 0;
+    if (op->family == FAM_ATTEND) return 0;  // its caches change from request to request
+    if (op->family == FAM_ROTARY) {
+        ptr[0] = op->sd.freq;
+        bytes[0] = 4 * op->sd.rot;
+        return op->sd.rot > 0 ? 1 : 0;
+    }
+    if (op->family == FAM_NORM) {
+        const miriam_seq_desc &q = op->sd;
+        for (const void *p : {(const void *)q.post, (const void *)q.pre, q.gate_kind == MIRIAM_GATE_CHANNEL ? q.gate : nullptr})
+            if (p) {
+                ptr[n] = p;
+                bytes[n++] = 4 * q.n;
+            }
+        return n;
+    }
     auto add = [&](const void *p, int64_t b) {
         if (p && b > 0 && n < 3) {
             ptr[n] = p;
@@ -979,6 +1012,37 @@ int miriam_op_create(const miriam_op_desc *d, miriam_op **out) { return op_creat
 
 int miriam_op_create_noalloc(const miriam_op_desc *d, miriam_op **out) { return op_create(d, out, true); }
 
+static int seq_op_create(const miriam_seq_desc *d, miriam_op **out, bool noalloc) {
+    if (!d || !out) return einval("null argument");
+    *out = nullptr;
+    miriam_op *op = new (std::nothrow) miriam_op();
+    if (!op) {
+        set_error("out of host memory");
+        return MIRIAM_ENOMEM;
+    }
+    op->sd = *d;
+    op->d.kind = d->kind;
+    op->d.dtype = d->dtype;
+    op->noalloc = noalloc;
+    if (hipGetDevice(&op->device) != hipSuccess) {
+        (void)hipGetLastError();
+        op->device = -1;
+    }
+    const int rc = create_seq(op);
+    if (rc != MIRIAM_OK) {
+        free_device(op);
+        delete op;
+        return rc;
+    }
+    query_occupancy(op);
+    *out = op;
+    return MIRIAM_OK;
+}
+
+int miriam_seq_op_create(const miriam_seq_desc *d, miriam_op **out) { return seq_op_create(d, out, false); }
+
+int miriam_seq_op_create_noalloc(const miriam_seq_desc *d, miriam_op **out) { return seq_op_create(d, out, true); }
+
 int miriam_op_query(const miriam_op *op, miriam_op_info *out) {
     if (!op || !out) return einval("null argument");
     std::memset(out, 0, sizeof(*out));
@@ -1001,7 +1065,7 @@ int miriam_op_query(const miriam_op *op, miriam_op_info *out) {
                     : op->lay == LAY_VEC || op->lay == LAY_PIPE || op->lay == LAY_PIPE_NB ? MIRIAM_PATH_DMA
                                              : MIRIAM_PATH_STAGED;
     else out->path = MIRIAM_PATH_OTHER;
-    out->ksplit = (op->family == FAM_IGEMM || op->family == FAM_SKINNY) ? op->ig.ksplit : 1;
+    out->ksplit = (op->family == FAM_IGEMM || op->family == FAM_SKINNY) ? op->ig.ksplit : op->family == FAM_ATTEND ? op->at.splits : 1;
     out->full_grid = op_full_grid(op);
     return MIRIAM_OK;
 }

@@ -105,4 +105,20 @@ int64_t miriam_plan_tree_head(int64_t T, int64_t cursor, int64_t max_len, int *d
     return e - b;
 }
 
+int miriam_plan_rotary_freqs(int64_t rot, double base, double factor, int64_t original, double low, double high,
+                             double *freq) {
+    if (rot < 2 || rot % 2 != 0 || !freq || !(base > 0.0) || !std::isfinite(base) || !(factor >= 1.0) || !std::isfinite(factor) ||
+        original < 0 || (original > 0 && !(low >= 0.0 && high > low))) {
+        miriam::set_error("rotary frequencies: rot even, base > 0, factor >= 1, original >= 0 and 0 <= low < high required");
+        return MIRIAM_EINVAL;
+    }
+    for (int64_t j = 0; j < rot / 2; ++j) {
+        const double f = std::pow(base, -2.0 * (double)j / (double)rot);
+        double keep = 0.0;  // share of the frequency that is not stretched
+        if (original > 0) keep = std::min(1.0, std::max(0.0, ((double)original * f / (2.0 * M_PI) - low) / (high - low)));
+        freq[j] = f * keep + f / factor * (1.0 - keep);
+    }
+    return MIRIAM_OK;
+}
+
 }  // extern "C"

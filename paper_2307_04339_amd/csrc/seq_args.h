@@ -1,0 +1,72 @@
+// Kernel argument blocks of the operators over packed token rows, passed by value.
+#pragma once
+
+#include "kargs.h"
+
+namespace miriam {
+
+// The norms around a block.
+struct NormArgs {
+    const void *x, *res, *gate;                      // res, gate: null = none
+    void *y, *z;                                     // either may be null
+    const float *post, *post_bias, *pre, *pre_bias;  // null = none
+    int64_t rows, n, ldx, ldr, ldg, ldy, ldz;
+    float scale, eps;
+    int32_t gate_kind;                               // miriam_gate
+    int32_t layer;                                   // 1: layer norm, 0: RMS norm
+};
+
+// What a row is divided into: one logical wave holding 1 or 2 vectors per lane; a tile's four logical waves
+// holding 1, 2, 4 or 8; or the tile's four reading the row again for each pass.
+enum NormForm { NORM_WAVE1 = 0, NORM_WAVE2 = 1, NORM_TILE1 = 2, NORM_TILE2 = 3, NORM_TILE4 = 4, NORM_TILE8 = 5, NORM_LONG = 6 };
+constexpr int norm_regs(int form) {
+    return form == NORM_WAVE1 || form == NORM_TILE1 ? 1 : form == NORM_WAVE2 || form == NORM_TILE2 ? 2 : form == NORM_TILE4 ? 4 : form == NORM_TILE8 ? 8 : 0;
+}
+
+// Sequences of packed rows over a paged cache (device arrays, clamped where they are read).
+struct SeqArgs {
+    const int32_t *q_start, *kv_len, *table;
+    int64_t tokens, seqs, ldt;
+    int64_t sp, sh, st;       // cache strides
+    int32_t page, pages, max_pages;
+    FastDiv fd_page;
+};
+
+struct RotaryArgs {
+    const void *x;
+    void *y, *k, *v;          // k, v: null without a cache
+    const double *freq;
+    SeqArgs sq;
+    int64_t ldx, ldy;
+    int32_t heads, kv_heads, d, rot;
+    int32_t interleaved;
+    int32_t items, rot_items; // vector pairs per head, and those of them that are turned
+    int32_t parts;            // logical waves per row
+    FastDiv fd_parts;         // division by it
+    float scale;
+};
+
+struct AttendArgs {
+    const void *x;
+    void *y;
+    const void *k, *v;
+    SeqArgs sq;
+    int64_t ldx, ldy;
+    int32_t heads, kv_heads, group, d;  // group = query heads per cache head
+    FastDiv fd_group, fd_kv, fd_splits; // division by group, kv_heads and splits
+    int32_t max_q, window, causal;
+    float scale;              // times log2(e): the exponentials are powers of two
+    int32_t splits;           // 1: every output is finished by one tile
+    int64_t T;
+    float *work;              // partial results
+    uint32_t work_bytes;
+    int32_t *counters;        // arrivals per output; back to 0 once a pass over the op completes
+};
+
+constexpr int kRowKeys = 128;    // keys of a block of the kernel for few query rows: 32 for each logical wave
+constexpr int kTileRows = 128;   // query rows of a tile of the kernel for many: 32 for each logical wave
+constexpr int kTileKeys = 64;    // and its keys per step
+// fp32 values of a partial result: rows x (dp values, maximum, sum)
+constexpr int64_t attend_partial(bool rows, int dp) { return (int64_t)(rows ? 16 : kTileRows) * (dp + 2); }
+
+}  // namespace miriam
