@@ -8,8 +8,10 @@
 // and the scores leave the first product in the layout in which the second takes them, if the contraction
 // index over the keys is numbered accordingly (it may be, as any order of the keys gives the same sum).
 //
-// fp16: P is 2^kShift times larger than a probability relative to the maximum (the sum as well, so it cancels):
-// values down to 2^-24 of the largest are then normal fp16 numbers.
+// The reference m need not be the maximum itself: it is raised only where the maximum is more than kRise (8) above it,
+// so the sums are seldom multiplied (for every other step of 64 random keys otherwise); P is then at most 2^8.
+// fp16: P is 2^kShift times larger (the sum as well, so it cancels): values down to 2^-20 of 2^m are then normal
+// fp16 numbers, and 2^(8 + 6) is one too.
 #pragma once
 
 #include "igemm.h"
@@ -18,11 +20,13 @@
 namespace miriam {
 
 template <class T> constexpr float kShift = 0.0f;
-template <> inline constexpr float kShift<half_t> = 10.0f;
+template <> inline constexpr float kShift<half_t> = 6.0f;
+constexpr float kRise = 8.0f;
 
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef __attribute__((address_space(3))) s16x4 *lds_s16x4;
+typedef __attribute__((address_space(3))) char *lds_char;
 
 // 16 bytes of zeros: where keys that are not there are read.
 static __device__ __attribute__((aligned(64))) uint32_t g_no_key[16];
@@ -63,6 +67,18 @@ __device__ __forceinline__ uint32_t pack2(float a, float b) {
 template <class T>
 __device__ __forceinline__ float unpack(uint32_t w, int hi) {
     return TypeOps<T>::to_f(__builtin_bit_cast(T, (uint16_t)(hi ? w >> 16 : w & 0xffffu)));
+}
+
+// s + the two 16-bit values of w.
+template <class T>
+__device__ __forceinline__ float add2(uint32_t w, float s) {
+    if constexpr (__is_same(T, half_t)) {
+        typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+        return __builtin_amdgcn_fdot2(__builtin_bit_cast(h2, w), __builtin_bit_cast(h2, 0x3c003c00u), s, false);
+    } else {
+        typedef __bf16 b2 __attribute__((ext_vector_type(2)));
+        return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(b2, w), __builtin_bit_cast(b2, 0x3f803f80u), s, false);
+    }
 }
 
 // Whether any of the eight 16-bit values is an infinity or a NaN.

@@ -3,8 +3,11 @@
 // A row is a (token, head of the group) pair, so the heads that share a cache head share its keys and values
 // in LDS, and a tile of a group of heads is short along the tokens, which wastes less at the causal edge.  Each
 // logical wave owns 32 rows: queries, running maximum, sum and the 32 x dp output stay in its registers.  64
-// keys and values at a time come by LDS-DMA into one of two stages while the other is used; their places in
-// the cache are looked up a step earlier by one wave.  One meeting per step.
+// keys and values at a time come by LDS-DMA into one of two stages while the other is used; the page table is read
+// a step earlier still.  One meeting per step.
+//
+// Where a load's rows (4 of 256 bytes) always lie in one page, its base is scalar and the lanes' offsets never
+// change (UNI); otherwise every lane finds its row by itself.
 //
 // Tiles of one cache head are consecutive, so a die's tiles share its L2's keys, and run from a sequence's last
 // rows to its first: the longest first.  With fewer than two tiles per CU a tile's keys are divided among
@@ -12,7 +15,7 @@
 #pragma once
 
 #include "attend.h"
-#include "igemm_dma.h"
+#include "tile_regs.h"
 
 namespace miriam {
 
@@ -23,14 +26,17 @@ struct TileKernel {
     static constexpr int CPR = DP / 8;        // 16-byte pieces of a row
     static constexpr int RPL = kWave / CPR;   // rows per load
     static constexpr int NLD = kTileKeys / RPL;  // loads per stage of keys (and of values)
-    static constexpr int STAGE = 2 * kTileKeys * DP * 2;
-    static constexpr int PL0 = 2 * STAGE, MASK0 = PL0 + 2 * kTileKeys * 8, LDS_BYTES = MASK0 + 16;
+    static constexpr int HALF = kTileKeys * DP * 2;  // a stage of keys or of values
+    static constexpr int LDS_BYTES = 4 * HALF;
+    static constexpr int NI = NLD / P;        // loads of a wave
+    // loads q of a wave whose rows are swizzled differently: q mod 4 (DP = 128), 2 (64), 8 (256)
+    static constexpr int CYC = DP == 64 ? 2 : DP == 128 ? 4 : 8, NSW = CYC / P > 0 ? CYC / P : 1;
     // pieces are exchanged so that what a read takes from several rows lies on different banks
     static constexpr __device__ int kswz(int r) { return DP == 64 ? (r >> 1) & 7 : r & 15; }
     static constexpr __device__ int vswz(int r) { return DP == 64 ? ((r >> 1) & 1) << 2 : (r & 3) << 2; }
 };
 
-template <class T, int DP, int P>
+template <class T, int DP, int P, bool UNI>
 __global__ __launch_bounds__(kWave * P, DP > 128 ? 1 : 2) void attend_tile_kernel(AttendArgs a, Shard sh) {
     typedef TileKernel<T, DP, P> K_;
     typedef Mfma<T, 32> MF;
@@ -39,12 +45,22 @@ __global__ __launch_bounds__(kWave * P, DP > 128 ? 1 : 2) void attend_tile_kerne
     constexpr int NJ = K_::NJ, ND = K_::ND, CPR = K_::CPR, RPL = K_::RPL, NLD = K_::NLD;
     __shared__ __attribute__((aligned(1024))) char smem[K_::LDS_BYTES];
     __shared__ int s_last;
+    lds_char const lsmem = (lds_char)smem;
+    // where the lane reads the values of output tile i in a stage, and the keys of step j: the swizzles go by the
+    // lane alone
+    const int xkey = (threadIdx.x % kWave) & 31, xhalf = (threadIdx.x % kWave) >> 5;
+    int vat[ND], kat[NJ];
+    {
+        const int l = threadIdx.x % kWave, vrow = 4 * xhalf + ((l >> 2) & 3), vpc = ((l >> 3) & 2) | ((l >> 1) & 1);
+#pragma unroll
+        for (int i = 0; i < ND; ++i) vat[i] = vrow * (DP * 2) + (((4 * i + vpc) ^ K_::vswz(vrow)) << 4) + ((l & 1) << 3);
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) kat[j] = xkey * (DP * 2) + (((2 * j + xhalf) ^ K_::kswz(xkey)) << 4);
+    }
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)smem;
     const int tid = threadIdx.x;
     const int pw = __builtin_amdgcn_readfirstlane(tid / kWave);
     const int lane = tid % kWave, hx = lane >> 5, xl = lane & 31;
-    int64_t *const places = reinterpret_cast<int64_t *>(smem + K_::PL0);      // [2][64]
-    uint64_t *const masks = reinterpret_cast<uint64_t *>(smem + K_::MASK0);   // [2]
     const T *const X = static_cast<const T *>(a.x);
     T *const Y = static_cast<T *>(a.y);
     const __amdgpu_buffer_rsrc_t rw = __builtin_amdgcn_make_buffer_rsrc(a.work, (short)0, (int)a.work_bytes, 0x00020000);
@@ -97,24 +113,84 @@ __global__ __launch_bounds__(kWave * P, DP > 128 ? 1 : 2) void attend_tile_kerne
         const int b0 = lo + (int)((int64_t)split * nb / a.splits), b1 = lo + (int)((int64_t)(split + 1) * nb / a.splits);
         const T *const kh = static_cast<const T *>(a.k) + (int64_t)hk * a.sq.sh, *const vh = static_cast<const T *>(a.v) + (int64_t)hk * a.sq.sh;
 
-        auto look_up = [&](int b) -> int64_t { return b < b1 ? key_place(a, s, tv, b * kTileKeys + lane) : -1; };
-        auto place = [&](int64_t pl, int buf) {
-            const uint64_t there = __ballot(pl >= 0);
-            places[buf * kTileKeys + lane] = pl;
-            if (lane == 0) masks[buf] = there;
-        };
-        // loads of the step whose places are in `buf` into stage `buf`
-        auto load = [&](int buf) {
+        // Page-table entries of a step: UNI: of its load (lane mod NLD), else of the lane's rows and of key `lane`.
+        constexpr int NE = UNI ? 1 : K_::NI + 1;
+        int32_t id[NE], slot_of[NE];
+        auto fetch = [&](int b) {
+            auto entry = [&](int j, int i) {
+                id[i] = -1;
+                slot_of[i] = 0;
+                if (b < b1 && j < tv.end && (UNI ? j + RPL > tv.begin : j >= tv.begin)) {
+                    const int pg = (int)fdiv((uint32_t)j, a.sq.fd_page);
+                    slot_of[i] = j - pg * a.sq.page;
+                    if (pg < a.sq.max_pages) id[i] = a.sq.table[s * a.sq.ldt + pg];
+                }
+            };
+            if constexpr (UNI) {
+                entry(b * kTileKeys + lane % NLD * RPL, 0);
+            } else {
 #pragma unroll
-            for (int i = 0; i < NLD / P; ++i) {
-                const int q = i * P + pw, r = q * RPL + lane / CPR;
-                const int64_t o = places[buf * kTileKeys + r];
-                const int dk = ((lane % CPR) ^ K_::kswz(r)) * 8, dv = ((lane % CPR) ^ K_::vswz(r)) * 8;
-                const T *none = reinterpret_cast<const T *>(g_no_key);
-                lds_dma16(o >= 0 && dk < a.d ? kh + o + dk : none, lds0 + (uint32_t)(buf * K_::STAGE + q * 1024));
-                lds_dma16(o >= 0 && dv < a.d ? vh + o + dv : none, lds0 + (uint32_t)(buf * K_::STAGE + kTileKeys * DP * 2 + q * 1024));
+                for (int i = 0; i < K_::NI; ++i) entry(b * kTileKeys + (i * P + pw) * RPL + lane / CPR, i);
+                entry(b * kTileKeys + lane, K_::NI);
             }
         };
+        // Where a step's keys and values lie (byte offsets, -1: nowhere), and which of its keys are there.
+        struct Where {
+            int64_t off[UNI ? 1 : K_::NI];
+            uint64_t there;
+        };
+        auto resolve = [&](int b) {
+            Where w;
+#pragma unroll
+            for (int i = 0; i < (UNI ? 1 : K_::NI); ++i) {
+                const bool ok = id[i] >= 0 && id[i] < a.sq.pages;
+                w.off[i] = ok ? (id[i] * a.sq.sp + (int64_t)slot_of[i] * a.sq.st) * 2 : -1;
+            }
+            if constexpr (UNI) {
+                const uint64_t groups = __ballot(w.off[0] >= 0);
+                constexpr uint64_t ALL = (1ull << NLD) - 1;
+                w.there = ~0ull;
+                if ((groups & ALL) != ALL || b * kTileKeys < tv.begin || (b + 1) * kTileKeys > tv.end) {
+                    const int j = b * kTileKeys + lane;
+                    w.there = __ballot(((groups >> (lane / RPL)) & 1) && j >= tv.begin && j < tv.end);
+                }
+            } else {
+                w.there = __ballot(id[K_::NI] >= 0 && id[K_::NI] < a.sq.pages);
+            }
+            return w;
+        };
+        // the lane's byte offsets within a load's rows
+        uint32_t ko[K_::NSW], vo[K_::NSW];
+        {
+            const int rr = lane / CPR;
+#pragma unroll
+            for (int w = 0; w < K_::NSW; ++w) {
+                const int r = (w * P + pw) * RPL + rr, row = UNI ? rr * (int)a.sq.st : 0;
+                const int dk = ((lane % CPR) ^ K_::kswz(r)) * 8, dv = ((lane % CPR) ^ K_::vswz(r)) * 8;
+                ko[w] = dk < a.d ? (uint32_t)((row + dk) * 2) : kOutOfRange;
+                vo[w] = dv < a.d ? (uint32_t)((row + dv) * 2) : kOutOfRange;
+            }
+        }
+        // loads of step b's keys or values (from `base`) into the stage at LDS byte `dst`; at: the lane's offsets
+        auto load = [&](int b, const Where &w, const T *base, const uint32_t (&at)[K_::NSW], uint32_t dst) {
+#pragma unroll
+            for (int i = 0; i < K_::NI; ++i) {
+                const int q = i * P + pw;
+                if constexpr (UNI) {
+                    const int32_t hi = __builtin_amdgcn_readlane((int)(w.off[0] >> 32), q);
+                    const uint64_t o = ((uint64_t)(uint32_t)hi << 32) | (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)w.off[0], q);
+                    const int n = clampi(tv.end - (b * kTileKeys + q * RPL), 0, RPL);  // rows up to the last key
+                    const uint32_t bytes = hi >= 0 ? (uint32_t)n * (uint32_t)a.sq.st * 2u : 0u;
+                    buf_dma16(at[i % K_::NSW], make_rsrc(reinterpret_cast<const char *>(base) + (hi >= 0 ? o : 0), bytes), 0u, dst + (uint32_t)(q * 1024));
+                } else {
+                    const uint32_t d = at[i % K_::NSW];
+                    const bool ok = w.off[i] >= 0 && d != kOutOfRange;
+                    lds_dma16(ok ? reinterpret_cast<const char *>(base) + w.off[i] + d : reinterpret_cast<const char *>(g_no_key), dst + (uint32_t)(q * 1024));
+                }
+            }
+        };
+        // keys: stages 0 and 1, values: stages 2 and 3 of kTileKeys rows each
+        auto stage = [&](int i) { return (uint32_t)(i * K_::HALF); };
 
         for (int slot = 0; slot < kLogicalWaves / P; ++slot) {
             const int lam = slot * P + pw;
@@ -138,84 +214,124 @@ __global__ __launch_bounds__(kWave * P, DP > 128 ? 1 : 2) void attend_tile_kerne
 #pragma unroll
             for (int i = 0; i < ND; ++i) acc[i] = acc_t{};
 
-            // one step on stage `buf`; edge: some rows do not see some of its keys
-            auto step = [&](int b, int buf, uint64_t there, bool edge) __attribute__((always_inline)) {
-                const char *const ks = smem + buf * K_::STAGE;
-                const uint32_t vs = lds0 + (uint32_t)(buf * K_::STAGE + kTileKeys * DP * 2);
-                acc_t sc[2];
+            // The step's work in pieces, for interleaving: while the matrix cores form the next step's scores, the
+            // vector units turn this one's into probabilities, and during the product with the values they look
+            // for the next scores' maximum.  Operands are read from LDS three pieces ahead.
+            constexpr int NQ = 2 * NJ, NP = 4 * ND, LA = 3;  // score and value products of a step
+            struct Scores {
+                acc_t s[2];
+            };
+            u32x4 op[LA + 1], p[2][2];
+            float top, sub;
+            lds_char kst, vst;
+            auto read = [&](auto n_) __attribute__((always_inline)) {
+                constexpr int n = decltype(n_)::value;
+                if constexpr (n < NQ) {
+                    op[n % (LA + 1)] = *(__attribute__((address_space(3))) u32x4 *)(kst + kat[n % NJ] + n / NJ * 32 * (DP * 2));
+                } else if constexpr (n < NQ + NP) {
+                    // eight keys of the lane's value in output tile i: those of step u of key tile kt
+                    constexpr int i = (n - NQ) % ND, u = (n - NQ) / ND % 2, kt = (n - NQ) / ND / 2;
 #pragma unroll
-                for (int kt = 0; kt < 2; ++kt) {
-                    sc[kt] = acc_t{};
-                    const int kr = 32 * kt + xl;
-#pragma unroll
-                    for (int j = 0; j < NJ; ++j) {
-                        const u32x4 k = *reinterpret_cast<const u32x4 *>(ks + kr * (DP * 2) + (((2 * j + hx) ^ K_::kswz(kr)) << 4));
-                        sc[kt] = MF::run(__builtin_bit_cast(op_t, k), __builtin_bit_cast(op_t, q[j]), sc[kt]);
+                    for (int j = 0; j < 2; ++j) {
+                        const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(vst + vat[i] + (32 * kt + 16 * u + 8 * j) * (DP * 2))));
+                        op[n % (LA + 1)][2 * j] = x[0];
+                        op[n % (LA + 1)][2 * j + 1] = x[1];
                     }
                 }
-                // lane: row xl, keys 64 b + 32 kt + 8 (i / 4) + 4 hx + i % 4
-                // key 32 kt + 8 (i / 4) + 4 hx + i % 4 is bit 8 (i / 4) + i % 4 of seen[kt]
-                if (edge) {
-                    const uint64_t w = (there & seen_keys(a, b * kTileKeys, pos)) >> (4 * hx);
-                    const uint32_t seen[2] = {(uint32_t)w, (uint32_t)(w >> 32)};
-#pragma unroll
-                    for (int kt = 0; kt < 2; ++kt)
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) sc[kt][i] = seen[kt] & (1u << (8 * (i / 4) + i % 4)) ? sc[kt][i] : -INFINITY;
-                }
-                float top = -INFINITY;
+            };
+            auto score = [&](auto n_, Scores &z) __attribute__((always_inline)) {
+                constexpr int n = decltype(n_)::value;
+                z.s[n / NJ] = MF::run(__builtin_bit_cast(op_t, op[n % (LA + 1)]), __builtin_bit_cast(op_t, q[n % NJ]), n % NJ == 0 ? acc_t{} : z.s[n / NJ]);
+            };
+            auto product = [&](auto n_) __attribute__((always_inline)) {
+                constexpr int n = decltype(n_)::value, i = n % ND, u = n / ND % 2, kt = n / ND / 2;
+                acc[i] = MF::run(__builtin_bit_cast(op_t, op[(NQ + n) % (LA + 1)]), __builtin_bit_cast(op_t, p[kt][u]), acc[i]);
+            };
+            // probabilities of pair w of the lane's 32 scores
+            auto power = [&](auto w_, const Scores &z) __attribute__((always_inline)) {
+                constexpr int w = decltype(w_)::value, kt = w / 8, i = w % 8;
+                const float p0 = exp2_(__builtin_fmaf(z.s[kt][2 * i], a.scale, -sub)), p1 = exp2_(__builtin_fmaf(z.s[kt][2 * i + 1], a.scale, -sub));
+                p[kt][i / 4][i % 4] = pack2<T>(p0, p1);
+                l = add2<T>(p[kt][i / 4][i % 4], l);
+            };
+            auto largest = [&](auto w_, const Scores &z) __attribute__((always_inline)) {
+                constexpr int w = decltype(w_)::value, kt = w / 8, i = w % 8;
+                top = fmaxf(fmaxf(z.s[kt][2 * i], z.s[kt][2 * i + 1]), top);
+            };
+            // f of the pairs that fall to piece n of N
+            auto share = [&](auto n_, auto N_, auto &&f) __attribute__((always_inline)) {
+                constexpr int n = decltype(n_)::value, N = decltype(N_)::value, w0 = n * 16 / N, w1 = (n + 1) * 16 / N;
+                static_for<w1 - w0>([&](auto w) { f(ActTag<w0 + decltype(w)::value>{}); });
+            };
+            // scores of keys that a row does not see; lane: row xl, key 32 kt + 8 (i / 4) + 4 hx + i % 4
+            auto mask = [&](int b, uint64_t there, Scores &z) __attribute__((always_inline)) {
+                const uint64_t w = (there & seen_keys(a, b * kTileKeys, pos)) >> (4 * hx);
+                const uint32_t seen[2] = {(uint32_t)w, (uint32_t)(w >> 32)};
 #pragma unroll
                 for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) top = fmaxf(top, sc[kt][i]);
-                {
-                    const uint32_t u = __builtin_bit_cast(uint32_t, top);
-                    const auto s32 = __builtin_amdgcn_permlane32_swap(u, u, false, false);
-                    top = fmaxf(__builtin_bit_cast(float, (uint32_t)s32[0]), __builtin_bit_cast(float, (uint32_t)s32[1]));
-                }
-                const float m1 = fmaxf(m, top * a.scale), ms = m1 == -INFINITY ? 0.0f : m1;
-                const float alpha = m == -INFINITY ? 1.0f : exp2_(m - ms);  // (nothing to lower before the first key)
-                m = m1;
-                if (__ballot(alpha != 1.0f)) {
+                    for (int i = 0; i < 16; ++i) z.s[kt][i] = seen[kt] & (1u << (8 * (i / 4) + i % 4)) ? z.s[kt][i] : -INFINITY;
+            };
+            // the reference that the next probabilities are relative to
+            auto raise = [&]() __attribute__((always_inline)) {
+                const uint32_t u = __builtin_bit_cast(uint32_t, top);
+                const auto s32 = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+                top = fmaxf(__builtin_bit_cast(float, (uint32_t)s32[0]), __builtin_bit_cast(float, (uint32_t)s32[1])) * a.scale;
+                if (__ballot(top > m + kRise)) {  // (-inf: the first key raises it)
+                    const float m1 = top > m + kRise ? top : m;
+                    const float alpha = m == m1 || m == -INFINITY ? 1.0f : exp2_(m - m1);  // (nothing to lower before the first key)
+                    m = m1;
                     l *= alpha;
 #pragma unroll
                     for (int i = 0; i < ND; ++i) acc[i] *= alpha;
                 }
-                u32x4 p[2][2];
-                const float sub = ms - kShift<T>;
-#pragma unroll
-                for (int kt = 0; kt < 2; ++kt)
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const float p0 = exp2_(__builtin_fmaf(sc[kt][2 * i], a.scale, -sub)), p1 = exp2_(__builtin_fmaf(sc[kt][2 * i + 1], a.scale, -sub));
-                        l += p0 + p1;
-                        p[kt][i / 4][i % 4] = pack2<T>(p0, p1);
-                    }
-                const int vrow = 4 * hx + ((lane >> 2) & 3), vpc = ((lane >> 3) & 2) | ((lane >> 1) & 1);
-                // eight keys of the lane's value in output tile i: those of step u of key tile kt
-                auto value = [&](int kt, int u, int i) __attribute__((always_inline)) {
-                    u32x4 v;
-#pragma unroll
-                    for (int j = 0; j < 2; ++j) {
-                        const int vr = 32 * kt + 16 * u + 8 * j + vrow;
-                        const uint32_t at = vs + (uint32_t)(vr * (DP * 2)) + (uint32_t)((((4 * i + vpc) ^ K_::vswz(vr)) << 4) + ((lane & 1) << 3));
-                        const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(uintptr_t)at));
-                        v[2 * j] = x[0];
-                        v[2 * j + 1] = x[1];
-                    }
-                    return v;
-                };
-#pragma unroll
-                for (int kt = 0; kt < 2; ++kt)
-#pragma unroll
-                    for (int u = 0; u < 2; ++u)
-#pragma unroll
-                        for (int i = 0; i < ND; ++i)
-                            acc[i] = MF::run(__builtin_bit_cast(op_t, value(kt, u, i)), __builtin_bit_cast(op_t, p[kt][u]), acc[i]);
+                sub = (m == -INFINITY ? 0.0f : m) - kShift<T>;
+            };
+            auto edge = [&](int b, uint64_t there) {  // some rows do not see some of its keys
+                const int kb = b * kTileKeys;
+                return ~there != 0 || (a.causal && kb + kTileKeys - 1 > pos_lo) || (a.window > 0 && kb <= pos_hi - a.window);
+            };
+            // The products of step b, whose scores are z, beside the scores of step b + 1 into zn.  One path for all
+            // steps (a branch around it costs registers, and the tile's other waves would wait all the same): scores
+            // of keys that are not there or that no row sees are masked, so their probabilities are 0 and the
+            // maximum goes without them, and their values are finite (see take_apart).
+            auto step = [&](int b, Scores &z, Scores &zn, uint64_t there1, int odd) __attribute__((always_inline)) {
+                kst = lsmem + stage(odd ^ 1);
+                vst = lsmem + stage(2 + odd);
+                top = -INFINITY;
+                static_for<LA>([&](auto n) { read(n); });
+                static_for<NQ>([&](auto n) {
+                    read(ActTag<decltype(n)::value + LA>{});
+                    score(n, zn);
+                    share(n, ActTag<NQ>{}, [&](auto w) { power(w, z); });
+                    __builtin_amdgcn_sched_barrier(0);
+                });
+                if (edge(b + 1, there1)) mask(b + 1, there1, zn);
+                static_for<NP>([&](auto n) {
+                    read(ActTag<NQ + decltype(n)::value + LA>{});
+                    product(n);
+                    share(n, ActTag<NP>{}, [&](auto w) { largest(w, zn); });
+                    __builtin_amdgcn_sched_barrier(0);
+                });
+                raise();
+            };
+            // scores of the first step
+            auto first = [&](int b, Scores &zn, uint64_t there1) __attribute__((always_inline)) {
+                kst = lsmem + stage(0);
+                top = -INFINITY;
+                static_for<LA>([&](auto n) { read(n); });
+                static_for<NQ>([&](auto n) {
+                    if constexpr (decltype(n)::value + LA < NQ) read(ActTag<decltype(n)::value + LA>{});
+                    score(n, zn);
+                    __builtin_amdgcn_sched_barrier(0);
+                });
+                if (edge(b, there1)) mask(b, there1, zn);
+                static_for<16>([&](auto w) { largest(w, zn); });
+                raise();
             };
             // infinities and NaN among the step's values, before its product
-            auto take_apart = [&](int kb, int buf, uint64_t there) __attribute__((always_inline)) {
-                char *const vb = smem + buf * K_::STAGE + kTileKeys * DP * 2;
+            auto take_apart = [&](int kb, int vst, uint64_t there) __attribute__((always_inline)) {
+                char *const vb = smem + stage(vst);
                 int bad = 0;
 #pragma unroll 1
                 for (int i = pw; i < NLD; i += P) bad |= not_finite<T>(*reinterpret_cast<const u32x4 *>(vb + i * 1024 + lane * 16));
@@ -243,39 +359,43 @@ __global__ __launch_bounds__(kWave * P, DP > 128 ? 1 : 2) void attend_tile_kerne
             };
 
             if (b0 < b1) {
-                int64_t pl = -1;
-                __syncthreads();  // the previous round's stages and places are free
-                if (pw == 0) {
-                    place(look_up(b0), 0);
-                    pl = look_up(b0 + 1);
-                }
+                Scores za, zb;
+                __syncthreads();  // the previous round's stages are free
+                fetch(b0);
+                Where w0 = resolve(b0);
+                fetch(b0 + 1);
+                load(b0, w0, kh, ko, lds0 + stage(0));
+                load(b0, w0, vh, vo, lds0 + stage(2));
+                uint64_t here = w0.there;  // keys of the step that are there
+                w0 = resolve(b0 + 1);
+                fetch(b0 + 2);
+                if (b0 + 1 < b1) load(b0 + 1, w0, kh, ko, lds0 + stage(1));
+                wait_vmcnt<0>();
                 __syncthreads();
-                load(0);
-                if (pw == 0) place(pl, 1);
-                for (int b = b0; b < b1; ++b) {
-                    const int buf = (b - b0) & 1;
-                    // this step's loads have arrived, the next one's places are written, and every wave is
-                    // done with the stage that the next one's loads go to
+                first(b0, za, here);
+                // step b's keys lie in stage b - b0 mod 2, its values in the like one.  Loads in flight during its
+                // products: keys of step b + 2, values of step b + 1, which w0 places.
+                auto turn = [&](int b, Scores &z, Scores &zn, int odd) __attribute__((always_inline)) {
+                    // step b + 1's keys and step b's values have arrived, and every wave is done with what the
+                    // loads to come overwrite
                     wait_vmcnt<0>();
                     __syncthreads();
-                    const uint64_t there_ = masks[buf];
-                    if (b + 1 < b1) load(buf ^ 1);
-                    if (pw == 0) pl = look_up(b + 2);
-                    const uint64_t there = ((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(there_ >> 32)) << 32) |
-                                           (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)there_);
+                    const Where w1 = resolve(b + 2);
+                    if (b + 2 < b1) load(b + 2, w1, kh, ko, lds0 + stage(odd));
+                    if (b + 1 < b1) load(b + 1, w0, vh, vo, lds0 + stage(2 + (odd ^ 1)));
+                    fetch(b + 3);
                     const int kb = b * kTileKeys;
                     // (the same for all waves: what the tile's first and last rows do not all see)
-                    if ((a.causal && kb + kTileKeys - 1 > tile_lo) || (a.window > 0 && kb <= tile_hi - a.window)) take_apart(kb, buf, there);
-                    const bool none = wrows <= 0 || (a.causal && kb > pos_hi) || (a.window > 0 && kb + kTileKeys - 1 <= pos_lo - a.window);
-                    if (!none) {
-                        const bool edge = ~there != 0 || (a.causal && kb + kTileKeys - 1 > pos_lo) || (a.window > 0 && kb <= pos_hi - a.window);
-                        step(b, buf, there, edge);
-                    }
-                    // places and mask of the step after the next: everyone has read those of this one
-                    if (b + 2 < b1) {
-                        __syncthreads();
-                        if (pw == 0) place(pl, buf);
-                    }
+                    if ((a.causal && kb + kTileKeys - 1 > tile_lo) || (a.window > 0 && kb <= tile_hi - a.window)) take_apart(kb, 2 + odd, here);
+                    step(b, z, zn, w0.there, odd);
+                    here = w0.there;
+                    w0 = w1;
+                };
+                for (int b = b0;;) {
+                    turn(b, za, zb, 0);
+                    if (++b >= b1) break;
+                    turn(b, zb, za, 1);
+                    if (++b >= b1) break;
                 }
             }
             // ---- the row's sum over both halves of the keys, then the output
@@ -360,12 +480,18 @@ __global__ __launch_bounds__(kWave * P, DP > 128 ? 1 : 2) void attend_tile_kerne
     }
 }
 
-template <class T, int DP>
-inline void tile_table(const void *out[3], int *lds) {
-    out[0] = reinterpret_cast<const void *>(&attend_tile_kernel<T, DP, 1>);
-    out[1] = reinterpret_cast<const void *>(&attend_tile_kernel<T, DP, 2>);
-    out[2] = reinterpret_cast<const void *>(&attend_tile_kernel<T, DP, 4>);
+template <class T, int DP, bool UNI>
+inline void tile_table_u(const void *out[3], int *lds) {
+    out[0] = reinterpret_cast<const void *>(&attend_tile_kernel<T, DP, 1, UNI>);
+    out[1] = reinterpret_cast<const void *>(&attend_tile_kernel<T, DP, 2, UNI>);
+    out[2] = reinterpret_cast<const void *>(&attend_tile_kernel<T, DP, 4, UNI>);
     *lds = TileKernel<T, DP, 4>::LDS_BYTES;
+}
+// uni: a load's 512 / dp rows lie in one page (the page a multiple of them) and span less than 2^31 bytes
+template <class T, int DP>
+inline void tile_table(bool uni, const void *out[3], int *lds) {
+    if (uni) tile_table_u<T, DP, true>(out, lds);
+    else tile_table_u<T, DP, false>(out, lds);
 }
 
 }  // namespace miriam

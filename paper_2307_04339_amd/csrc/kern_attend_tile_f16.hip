@@ -2,11 +2,11 @@
 #include "attend_tile.h"
 
 namespace miriam {
-int attend_tile_kernels_f16(int dp, const void *out[3], int *lds) {
+int attend_tile_kernels_f16(int dp, bool uni, const void *out[3], int *lds) {
     switch (dp) {
-    case 64: tile_table<half_t, 64>(out, lds); return 0;
-    case 128: tile_table<half_t, 128>(out, lds); return 0;
-    case 256: tile_table<half_t, 256>(out, lds); return 0;
+    case 64: tile_table<half_t, 64>(uni, out, lds); return 0;
+    case 128: tile_table<half_t, 128>(uni, out, lds); return 0;
+    case 256: tile_table<half_t, 256>(uni, out, lds); return 0;
     default: return -1;
     }
 }

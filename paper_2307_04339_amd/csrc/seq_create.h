@@ -251,8 +251,10 @@ static int create_attention(miriam_op *op) {
     if (op->T >= (int64_t)INT32_MAX) return einval("attention: too large for 32-bit tile indexing");
     a.fd_splits = make_fastdiv((uint32_t)a.splits);
     a.T = op->T;
-    const bool f16 = d.dtype == MIRIAM_F16;
-    if ((rows ? (f16 ? attend_rows_kernels_f16 : attend_rows_kernels_bf16) : (f16 ? attend_tile_kernels_f16 : attend_tile_kernels_bf16))(dp, op->kern, &op->lds_bytes) != 0)
+    // many rows: the rows of one load (512 / dp keys) always in one page
+    const bool f16 = d.dtype == MIRIAM_F16, uni = d.page % (512 / dp) == 0 && d.cache_token < ((int64_t)1 << 26);
+    if ((rows ? (f16 ? attend_rows_kernels_f16(dp, op->kern, &op->lds_bytes) : attend_rows_kernels_bf16(dp, op->kern, &op->lds_bytes))
+              : (f16 ? attend_tile_kernels_f16(dp, uni, op->kern, &op->lds_bytes) : attend_tile_kernels_bf16(dp, uni, op->kern, &op->lds_bytes))) != 0)
         return einval("attention: no kernel for this dtype");
     // at full capacity
     op->flops = 4.0 * (double)d.tokens * (double)width * (double)keys;
