@@ -290,7 +290,7 @@ __global__ __launch_bounds__(kWave * P, DP > 128 ? 1 : 2) void attend_rows_kerne
                 put(r, d4, o, l);
             } else {
                 // device-coherent stores: another die's tile may join them
-                const uint32_t at = (uint32_t)slot0 * (uint32_t)(attend_partial(true, DP) * 4);
+                const uint32_t at = (uint32_t)slot0 * (uint32_t)(attend_partial(16, DP) * 4);
                 __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, o), rw, (int)(at + (uint32_t)(r * DP + d4) * 4u), 0, kAgent);
                 if (d4 == 0) {
                     __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(uint32_t, m), rw, (int)(at + (uint32_t)(16 * DP + r) * 4u), 0, kAgent);
@@ -321,7 +321,7 @@ __global__ __launch_bounds__(kWave * P, DP > 128 ? 1 : 2) void attend_rows_kerne
 #pragma unroll
                         for (int q = 0; q < NB; ++q) {
                             const int wq = w + q <= w1 ? w + q : w1;
-                            const uint32_t at = (uint32_t)(wq * 2 + (wq == w0 ? 1 : 0)) * (uint32_t)(attend_partial(true, DP) * 4);
+                            const uint32_t at = (uint32_t)(wq * 2 + (wq == w0 ? 1 : 0)) * (uint32_t)(attend_partial(16, DP) * 4);
                             ow[q] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(rw, (int)(at + (uint32_t)(r * DP + d4) * 4u), 0, kAgent));
                             mw[q] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rw, (int)(at + (uint32_t)(16 * DP + r) * 4u), 0, kAgent));
                             lw[q] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rw, (int)(at + (uint32_t)(16 * DP + 16 + r) * 4u), 0, kAgent));

@@ -1,9 +1,10 @@
-// Attention over a paged cache for many query rows: tiles of 128 rows, bound by the matrix cores.
+// Attention over a paged cache for many query rows: tiles of 128 rows, bound by the matrix cores and by what they
+// are fed from LDS.
 //
 // A row is a (token, head of the group) pair, so the heads that share a cache head share its keys and values
 // in LDS, and a tile of a group of heads is short along the tokens, which wastes less at the causal edge.  Each
-// logical wave owns 32 rows: queries, running maximum, sum and the 32 x dp output stay in its registers.  64
-// keys and values at a time come by LDS-DMA into one of two stages while the other is used; the page table is read
+// logical wave owns 32 rows: queries, running maximum, sum and output stay in its registers.  64 keys and values
+// at a time come by LDS-DMA into one of two stages while the other is used; the page table is read
 // a step earlier still.  One meeting per step.
 //
 // Where a load's rows (4 of 256 bytes) always lie in one page, its base is scalar and the lanes' offsets never
@@ -214,10 +215,11 @@ __global__ __launch_bounds__(kWave * P, DP > 128 ? 1 : 2) void attend_tile_kerne
 #pragma unroll
             for (int i = 0; i < ND; ++i) acc[i] = acc_t{};
 
-            // The step's work in pieces, for interleaving: while the matrix cores form the next step's scores, the
-            // vector units turn this one's into probabilities, and during the product with the values they look
-            // for the next scores' maximum.  Operands are read from LDS three pieces ahead.
-            constexpr int NQ = 2 * NJ, NP = 4 * ND, LA = 3;  // score and value products of a step
+            // The step's work in pieces.  The next step's scores are formed before this step's are turned into
+            // probabilities, so that the vector units start on those while the matrix cores still work on these;
+            // beside the products with the values they look for the next scores' maximum.  (Powers beside every
+            // product of the next scores instead: 2% slower.)  Operands are read from LDS three pieces ahead.
+            constexpr int NQ = 2 * NJ, NP = 4 * ND, NW = 16, LA = 3;  // operands of the scores and of the values, pairs of scores of a lane
             struct Scores {
                 acc_t s[2];
             };
@@ -240,14 +242,14 @@ __global__ __launch_bounds__(kWave * P, DP > 128 ? 1 : 2) void attend_tile_kerne
                 }
             };
             auto score = [&](auto n_, Scores &z) __attribute__((always_inline)) {
-                constexpr int n = decltype(n_)::value;
-                z.s[n / NJ] = MF::run(__builtin_bit_cast(op_t, op[n % (LA + 1)]), __builtin_bit_cast(op_t, q[n % NJ]), n % NJ == 0 ? acc_t{} : z.s[n / NJ]);
+                constexpr int n = decltype(n_)::value, kt = n / NJ;
+                z.s[kt] = MF::run(__builtin_bit_cast(op_t, op[n % (LA + 1)]), __builtin_bit_cast(op_t, q[n % NJ]), n % NJ == 0 ? acc_t{} : z.s[kt]);
             };
             auto product = [&](auto n_) __attribute__((always_inline)) {
                 constexpr int n = decltype(n_)::value, i = n % ND, u = n / ND % 2, kt = n / ND / 2;
                 acc[i] = MF::run(__builtin_bit_cast(op_t, op[(NQ + n) % (LA + 1)]), __builtin_bit_cast(op_t, p[kt][u]), acc[i]);
             };
-            // probabilities of pair w of the lane's 32 scores
+            // probabilities of pair w of the lane's scores, in the order in which the products take them
             auto power = [&](auto w_, const Scores &z) __attribute__((always_inline)) {
                 constexpr int w = decltype(w_)::value, kt = w / 8, i = w % 8;
                 const float p0 = exp2_(__builtin_fmaf(z.s[kt][2 * i], a.scale, -sub)), p1 = exp2_(__builtin_fmaf(z.s[kt][2 * i + 1], a.scale, -sub));
@@ -257,11 +259,6 @@ __global__ __launch_bounds__(kWave * P, DP > 128 ? 1 : 2) void attend_tile_kerne
             auto largest = [&](auto w_, const Scores &z) __attribute__((always_inline)) {
                 constexpr int w = decltype(w_)::value, kt = w / 8, i = w % 8;
                 top = fmaxf(fmaxf(z.s[kt][2 * i], z.s[kt][2 * i + 1]), top);
-            };
-            // f of the pairs that fall to piece n of N
-            auto share = [&](auto n_, auto N_, auto &&f) __attribute__((always_inline)) {
-                constexpr int n = decltype(n_)::value, N = decltype(N_)::value, w0 = n * 16 / N, w1 = (n + 1) * 16 / N;
-                static_for<w1 - w0>([&](auto w) { f(ActTag<w0 + decltype(w)::value>{}); });
             };
             // scores of keys that a row does not see; lane: row xl, key 32 kt + 8 (i / 4) + 4 hx + i % 4
             auto mask = [&](int b, uint64_t there, Scores &z) __attribute__((always_inline)) {
@@ -303,14 +300,15 @@ __global__ __launch_bounds__(kWave * P, DP > 128 ? 1 : 2) void attend_tile_kerne
                 static_for<NQ>([&](auto n) {
                     read(ActTag<decltype(n)::value + LA>{});
                     score(n, zn);
-                    share(n, ActTag<NQ>{}, [&](auto w) { power(w, z); });
                     __builtin_amdgcn_sched_barrier(0);
                 });
                 if (edge(b + 1, there1)) mask(b + 1, there1, zn);
-                static_for<NP>([&](auto n) {
-                    read(ActTag<NQ + decltype(n)::value + LA>{});
-                    product(n);
-                    share(n, ActTag<NP>{}, [&](auto w) { largest(w, zn); });
+                static_for<NW>([&](auto w) { power(w, z); });
+                static_for<NP>([&](auto n_) {
+                    constexpr int n = decltype(n_)::value, w0 = n * NW / NP, w1 = (n + 1) * NW / NP;
+                    read(ActTag<NQ + n + LA>{});
+                    product(n_);
+                    static_for<w1 - w0>([&](auto w) { largest(ActTag<w0 + decltype(w)::value>{}, zn); });
                     __builtin_amdgcn_sched_barrier(0);
                 });
                 raise();
@@ -326,7 +324,7 @@ __global__ __launch_bounds__(kWave * P, DP > 128 ? 1 : 2) void attend_tile_kerne
                     __builtin_amdgcn_sched_barrier(0);
                 });
                 if (edge(b, there1)) mask(b, there1, zn);
-                static_for<16>([&](auto w) { largest(w, zn); });
+                static_for<NW>([&](auto w) { largest(w, zn); });
                 raise();
             };
             // infinities and NaN among the step's values, before its product
@@ -398,16 +396,15 @@ __global__ __launch_bounds__(kWave * P, DP > 128 ? 1 : 2) void attend_tile_kerne
                     if (++b >= b1) break;
                 }
             }
-            // ---- the row's sum over both halves of the keys, then the output
+            // ---- the rows' sums over both halves of the keys, then the output
             {
                 const uint32_t u = __builtin_bit_cast(uint32_t, l);
                 const auto s32 = __builtin_amdgcn_permlane32_swap(u, u, false, false);
                 l = __builtin_bit_cast(float, (uint32_t)s32[0]) + __builtin_bit_cast(float, (uint32_t)s32[1]);
-            }
-            if (a.splits <= 1) {
-                const float inv = l > 0.0f || l != l ? 1.0f / l : 0.0f;  // no key: zeros
-                T *yr = Y + (int64_t)(sv.q0 + tok) * a.ldy + (int64_t)(hk * g + r - tok * g) * a.d;
-                if (xl < wrows) {
+                if (xl >= wrows) {
+                } else if (a.splits <= 1) {
+                    const float inv = l > 0.0f || l != l ? 1.0f / l : 0.0f;  // no key: zeros
+                    T *yr = Y + (int64_t)(sv.q0 + tok) * a.ldy + (int64_t)(hk * g + r - tok * g) * a.d;
 #pragma unroll
                     for (int i = 0; i < ND; ++i)
 #pragma unroll
@@ -419,18 +416,16 @@ __global__ __launch_bounds__(kWave * P, DP > 128 ? 1 : 2) void attend_tile_kerne
                             w[1] = pack2<T>(acc[i][4 * c + 2] * inv, acc[i][4 * c + 3] * inv);
                             *reinterpret_cast<u32x2 *>(yr + d) = w;
                         }
-                }
-            } else {
-                // partial result, device-coherent: another die's tile may join it
-                const uint32_t at = (uint32_t)t * (uint32_t)(attend_partial(false, DP) * 4), pr = (uint32_t)(32 * lam + xl);
-                if (xl < wrows) {
+                } else {
+                    // partial result as the lanes hold it, device-coherent: another die's tile may join it
+                    const uint32_t at = (uint32_t)t * (uint32_t)(attend_partial(kTileRows, DP) * 4), pr = (uint32_t)(32 * lam + xl);
 #pragma unroll
                     for (int i = 0; i < ND; ++i)
 #pragma unroll
                         for (int c = 0; c < 4; ++c) {
-                            const uint32_t d = (uint32_t)(32 * i + 8 * c + 4 * hx);
+                            if (32 * i + 8 * c >= a.d) continue;
                             const f32x4 o = {acc[i][4 * c], acc[i][4 * c + 1], acc[i][4 * c + 2], acc[i][4 * c + 3]};
-                            __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, o), rw, (int)(at + (pr * DP + d) * 4u), 0, kAgent);
+                            __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, o), rw, (int)(at + (uint32_t)(((lam * ND + i) * 4 + c) * kWave + lane) * 16u), 0, kAgent);
                         }
                     if (hx == 0) {
                         __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(uint32_t, m), rw, (int)(at + (kTileRows * DP + pr) * 4u), 0, kAgent);
@@ -450,29 +445,62 @@ __global__ __launch_bounds__(kWave * P, DP > 128 ? 1 : 2) void attend_tile_kerne
             }
             __syncthreads();
             if (s_last) {
-                const int n4 = a.d / 4;
-                for (int i = tid; i < rows * n4; i += kWave * P) {
-                    const int r = i / n4, d4 = (i - r * n4) * 4;
-                    float m = -INFINITY, l = 0.0f;
-                    f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
+                // each split's share of each row's sum, in LDS (the stages are free); then the outputs, the loads of
+                // several of a thread in flight
+                float *const weight = reinterpret_cast<float *>(smem);  // [splits][kTileRows]
+                const uint32_t part = (uint32_t)(attend_partial(kTileRows, DP) * 4), at0 = (uint32_t)out * (uint32_t)a.splits * part;
+                auto word = [&](int w, uint32_t i) {
+                    return __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rw, (int)(at0 + (uint32_t)w * part + i * 4u), 0, kAgent));
+                };
+                for (int r = tid; r < rows; r += kWave * P) {
+                    float top = -INFINITY, sum = 0.0f;
                     for (int w = 0; w < a.splits; ++w) {
-                        const uint32_t at = (uint32_t)(out * a.splits + w) * (uint32_t)(attend_partial(false, DP) * 4);
-                        const f32x4 ow = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(rw, (int)(at + (uint32_t)(r * DP + d4) * 4u), 0, kAgent));
-                        const float mw = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rw, (int)(at + (uint32_t)(kTileRows * DP + r) * 4u), 0, kAgent));
-                        const float lw = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rw, (int)(at + (uint32_t)(kTileRows * (DP + 1) + r) * 4u), 0, kAgent));
-                        const float top = fmaxf(m, mw), ms = top == -INFINITY ? 0.0f : top, f0 = exp2_(m - ms), f = exp2_(mw - ms);
-                        m = top;
-                        l = __builtin_fmaf(f, lw, l * f0);
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) o[e] = __builtin_fmaf(f, ow[e], o[e] * f0);
+                        const float mw = word(w, (uint32_t)(kTileRows * DP + r));
+                        weight[w * kTileRows + r] = mw;
+                        top = fmaxf(top, mw);
                     }
-                    const float inv = l > 0.0f || l != l ? 1.0f / l : 0.0f;
-                    const int tok = (int)fdiv((uint32_t)(row0 + r), a.fd_group);
-                    T *yr = Y + (int64_t)(sv.q0 + tok) * a.ldy + (int64_t)(hk * g + row0 + r - tok * g) * a.d + d4;
-                    u32x2 w;
-                    w[0] = pack2<T>(o[0] * inv, o[1] * inv);
-                    w[1] = pack2<T>(o[2] * inv, o[3] * inv);
-                    *reinterpret_cast<u32x2 *>(yr) = w;
+                    const float ms = top == -INFINITY ? 0.0f : top;
+                    for (int w = 0; w < a.splits; ++w) {
+                        const float f = exp2_(weight[w * kTileRows + r] - ms);
+                        weight[w * kTileRows + r] = f;
+                        sum = __builtin_fmaf(f, word(w, (uint32_t)(kTileRows * (DP + 1) + r)), sum);
+                    }
+                    const float inv = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
+                    for (int w = 0; w < a.splits; ++w) weight[w * kTileRows + r] *= inv;
+                }
+                __syncthreads();
+                // piece i of a partial result: values 32 (i / 256 % ND) + 8 (i / 64 % 4) + 4 (i / 32 % 2) .. of row
+                // 32 (i / (256 ND)) + i % 32
+                constexpr int PIECES = kTileRows * DP / 4, step = kWave * P, NB = 8;
+                for (int i0 = tid; i0 < PIECES; i0 += NB * step) {
+                    f32x4 o[NB];
+#pragma unroll
+                    for (int j = 0; j < NB; ++j) o[j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+                    auto row_of = [&](int j) { return 32 * ((i0 + j * step) / (256 * ND)) + (i0 + j * step) % 32; };
+                    auto col_of = [&](int j) { return 32 * ((i0 + j * step) / 256 % ND) + 8 * ((i0 + j * step) / 64 % 4) + 4 * ((i0 + j * step) / 32 % 2); };
+                    for (int w = 0; w < a.splits; ++w) {
+                        f32x4 ow[NB];
+#pragma unroll
+                        for (int j = 0; j < NB; ++j)  // (rows and values that are not there lie in the workspace, too)
+                            ow[j] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(rw, (int)(at0 + (uint32_t)w * part + (uint32_t)(i0 + j * step) * 16u), 0, kAgent));
+#pragma unroll
+                        for (int j = 0; j < NB; ++j) {
+                            const float f = weight[w * kTileRows + row_of(j)];
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) o[j][e] = __builtin_fmaf(f, ow[j][e], o[j][e]);
+                        }
+                    }
+#pragma unroll
+                    for (int j = 0; j < NB; ++j) {
+                        const int rj = row_of(j), d = col_of(j);
+                        if (rj >= rows || d >= a.d) continue;
+                        const int tok = (int)fdiv((uint32_t)(row0 + rj), a.fd_group);
+                        T *yr = Y + (int64_t)(sv.q0 + tok) * a.ldy + (int64_t)(hk * g + row0 + rj - tok * g) * a.d + d;
+                        u32x2 w;
+                        w[0] = pack2<T>(o[j][0], o[j][1]);
+                        w[1] = pack2<T>(o[j][2], o[j][3]);
+                        *reinterpret_cast<u32x2 *>(yr) = w;
+                    }
                 }
             }
             __syncthreads();  // s_last is free

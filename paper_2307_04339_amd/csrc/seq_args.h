@@ -67,6 +67,6 @@ constexpr int kRowKeys = 128;    // keys of a block of the kernel for few query 
 constexpr int kTileRows = 128;   // query rows of a tile of the kernel for many: 32 for each logical wave
 constexpr int kTileKeys = 64;    // and its keys per step
 // fp32 values of a partial result: rows x (dp values, maximum, sum)
-constexpr int64_t attend_partial(bool rows, int dp) { return (int64_t)(rows ? 16 : kTileRows) * (dp + 2); }
+constexpr int64_t attend_partial(int rows, int dp) { return (int64_t)rows * (dp + 2); }
 
 }  // namespace miriam

@@ -208,7 +208,7 @@ static int create_attention(miriam_op *op) {
     a.scale = (float)((double)d.scale * 1.4426950408889634074);
     const bool rows = (int64_t)a.max_q * a.group <= 16;
     const int dp = d.head_dim <= 64 ? 64 : d.head_dim <= 128 ? 128 : 256;
-    const int64_t cus = device_cus(), part = attend_partial(rows, dp) * 4, keys = d.page * d.max_pages;
+    const int64_t cus = device_cus(), part = attend_partial(rows ? 16 : kTileRows, dp) * 4, keys = d.page * d.max_pages;
     int64_t outputs;  // outputs that several tiles may share
     int64_t slots;    // partial results in the workspace
     if (rows) {
@@ -224,7 +224,7 @@ static int create_attention(miriam_op *op) {
         const int64_t qt = std::min(d.tokens * a.group / kTileRows + d.seqs, d.seqs * cdiv((int64_t)a.max_q * a.group, kTileRows));
         if (qt >= kMost / d.kv_heads) return einval("attention: too large for 32-bit tile indexing");
         outputs = qt * d.kv_heads;
-        a.splits = (int32_t)std::max<int64_t>(1, std::min<int64_t>(2 * cus / outputs, cdiv(keys, 4 * kTileKeys)));
+        a.splits = (int32_t)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(2 * cus / outputs, 64), cdiv(keys, 4 * kTileKeys)));
         op->T = outputs * a.splits;
         slots = op->T;
     }
