@@ -34,6 +34,7 @@ struct RowsKernel {
 
 template <class T, int DP, int P>
 __global__ __launch_bounds__(kWave * P, DP > 128 ? 1 : 2) void attend_rows_kernel(AttendArgs a, Shard sh) {
+    constexpr int kJoin = 16;  // partial results joined at once
     typedef RowsKernel<T, DP, P> K_;
     typedef Mfma<T, 16> MF;
     typedef typename MF::op_t op_t;
@@ -66,16 +67,92 @@ __global__ __launch_bounds__(kWave * P, DP > 128 ? 1 : 2) void attend_rows_kerne
         const int n = (v.end + kRowKeys - 1) / kRowKeys - v.begin / kRowKeys;
         return n > 0 ? n : 1;
     };
-    // all blocks, and each tile's share
+    // All blocks, and each tile's share.  While there are tiles enough for runs of two blocks that do not cross
+    // from one head into the next, these are taken (a head's list then counts as even): two blocks take little
+    // longer than one, and most heads of short sequences need no joining.
     int total = 0, share = 0;
+    bool even = false;
     if (a.splits > 1) {
-        int sum = 0;
+        int sum = 0, pairs = 0;
 #pragma unroll 4
-        for (int s = lane; s < seqs; s += kWave) sum += blocks_of(s);
-        for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
+        for (int s = lane; s < seqs; s += kWave) {
+            const int n = blocks_of(s);
+            sum += n;
+            pairs += (n + 1) / 2;
+        }
+        for (int o = 32; o > 0; o >>= 1) {
+            sum += __shfl_xor(sum, o);
+            pairs += __shfl_xor(pairs, o);
+        }
         total = __builtin_amdgcn_readfirstlane(sum) * heads;
-        share = (total + (int)a.T - 1) / (int)a.T;
+        pairs = __builtin_amdgcn_readfirstlane(pairs) * heads;
+        even = pairs <= (int)a.T;
+        if (even) total = 2 * pairs;
+        share = even ? 2 : (total + (int)a.T - 1) / (int)a.T;
     }
+    auto list_of = [&](int s) {  // places of a head of sequence s in the list
+        const int n = blocks_of(s);
+        return even ? (n + 1) & ~1 : n;
+    };
+
+    // A partial result into `slot` of the workspace, by device-coherent stores: another die's tile may join it.
+    auto keep = [&](int slot, int r, int d4, const f32x4 &o, float m, float l) {
+        const uint32_t at = (uint32_t)slot * (uint32_t)(attend_partial(16, DP) * 4);
+        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, o), rw, (int)(at + (uint32_t)(r * DP + d4) * 4u), 0, kAgent);
+        if (d4 == 0) {
+            __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(uint32_t, m), rw, (int)(at + (uint32_t)(16 * DP + r) * 4u), 0, kAgent);
+            __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(uint32_t, l), rw, (int)(at + (uint32_t)(16 * DP + 16 + r) * 4u), 0, kAgent);
+        }
+    };
+    // Whether this tile is the last of n to arrive at `counter`; its stores are complete before it is counted.
+    auto arrive = [&](int32_t *counter, int n) {
+        __builtin_amdgcn_s_waitcnt(0);
+        __syncthreads();
+        if (tid == 0) {
+            const int prev = __hip_atomic_fetch_add(counter, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            s_last = prev == n - 1;
+            if (s_last) __hip_atomic_store(counter, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        }
+        __syncthreads();
+        return s_last != 0;
+    };
+    // Partial results slot_of(0 .. n - 1) joined in order, 16 loads in flight; done(row, d, o, m, l) for each piece.
+    auto join = [&](int rows, int n, auto &&slot_of, auto &&done) __attribute__((always_inline)) {
+        const int n4 = a.d / 4;
+        for (int i = tid; i < rows * n4; i += kWave * P) {
+            const int r = i / n4, d4 = (i - r * n4) * 4;
+            float m = -INFINITY, l = 0.0f;
+            f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
+            for (int w = 0; w < n; w += kJoin) {
+                f32x4 ow[kJoin];
+                float mw[kJoin], lw[kJoin];
+#pragma unroll
+                for (int q = 0; q < kJoin; ++q) {
+                    const uint32_t at = (uint32_t)slot_of(w + q < n ? w + q : n - 1) * (uint32_t)(attend_partial(16, DP) * 4);
+                    ow[q] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(rw, (int)(at + (uint32_t)(r * DP + d4) * 4u), 0, kAgent));
+                    mw[q] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rw, (int)(at + (uint32_t)(16 * DP + r) * 4u), 0, kAgent));
+                    lw[q] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rw, (int)(at + (uint32_t)(16 * DP + 16 + r) * 4u), 0, kAgent));
+                }
+                float top = m;
+#pragma unroll
+                for (int q = 0; q < kJoin; ++q) top = fmaxf(top, mw[q]);
+                const float ms = top == -INFINITY ? 0.0f : top, f0 = exp2_(m - ms);
+                m = top;
+                l *= f0;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[e] *= f0;
+#pragma unroll
+                for (int q = 0; q < kJoin; ++q) {
+                    if (w + q >= n) continue;
+                    const float f = exp2_(mw[q] - ms);
+                    l = __builtin_fmaf(f, lw[q], l);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) o[e] = __builtin_fmaf(f, ow[q][e], o[e]);
+                }
+            }
+            done(r, d4, o, m, l);
+        }
+    };
 
     // One run: blocks [b0, b1) of the nb of cache head hk of sequence s, the first of which is block `first`
     // of the sequence; tiles w0 .. w1 share the head.
@@ -260,7 +337,7 @@ __global__ __launch_bounds__(kWave * P, DP > 128 ? 1 : 2) void attend_rows_kerne
         // ---- the four logical waves' results, in order
         const bool whole = w0 == w1;
         const int slot0 = (int)t * 2 + (t == w0 ? 1 : 0);
-        auto put = [&](int r, int d4, const f32x4 &o, float l) {
+        auto put = [&](int r, int d4, const f32x4 &o, float, float l) {
             const int tok = (int)fdiv((uint32_t)r, a.fd_group);
             T *yr = Y + (int64_t)(sv.q0 + tok) * a.ldy + (int64_t)(hk * g + r - tok * g) * a.d + d4;
             const float inv = l > 0.0f || l != l ? 1.0f / l : 0.0f;  // no key: zeros
@@ -286,64 +363,23 @@ __global__ __launch_bounds__(kWave * P, DP > 128 ? 1 : 2) void attend_rows_kerne
 #pragma unroll
                 for (int e = 0; e < 4; ++e) o[e] = __builtin_fmaf(f, ow[e], o[e]);
             }
-            if (whole) {
-                put(r, d4, o, l);
-            } else {
-                // device-coherent stores: another die's tile may join them
-                const uint32_t at = (uint32_t)slot0 * (uint32_t)(attend_partial(16, DP) * 4);
-                __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, o), rw, (int)(at + (uint32_t)(r * DP + d4) * 4u), 0, kAgent);
-                if (d4 == 0) {
-                    __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(uint32_t, m), rw, (int)(at + (uint32_t)(16 * DP + r) * 4u), 0, kAgent);
-                    __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(uint32_t, l), rw, (int)(at + (uint32_t)(16 * DP + 16 + r) * 4u), 0, kAgent);
-                }
-            }
+            if (whole) put(r, d4, o, m, l);
+            else keep(slot0, r, d4, o, m, l);
         }
         if (!whole) {
-            // the partial result's stores complete before the arrival is counted
-            __builtin_amdgcn_s_waitcnt(0);
-            __syncthreads();
-            if (tid == 0) {
-                int32_t *const c = a.counters + (int64_t)s * heads + hk;
-                const int prev = __hip_atomic_fetch_add(c, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-                s_last = prev == w1 - w0;
-                if (s_last) __hip_atomic_store(c, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            }
-            __syncthreads();
-            if (s_last) {
-                for (int i = tid; i < rows * n4; i += kWave * P) {
-                    const int r = i / n4, d4 = (i - r * n4) * 4;
-                    float m = -INFINITY, l = 0.0f;
-                    f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
-                    constexpr int NB = 8;
-                    for (int w = w0; w <= w1; w += NB) {
-                        f32x4 ow[NB];
-                        float mw[NB], lw[NB];
-#pragma unroll
-                        for (int q = 0; q < NB; ++q) {
-                            const int wq = w + q <= w1 ? w + q : w1;
-                            const uint32_t at = (uint32_t)(wq * 2 + (wq == w0 ? 1 : 0)) * (uint32_t)(attend_partial(16, DP) * 4);
-                            ow[q] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(rw, (int)(at + (uint32_t)(r * DP + d4) * 4u), 0, kAgent));
-                            mw[q] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rw, (int)(at + (uint32_t)(16 * DP + r) * 4u), 0, kAgent));
-                            lw[q] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rw, (int)(at + (uint32_t)(16 * DP + 16 + r) * 4u), 0, kAgent));
-                        }
-                        float top = m;
-#pragma unroll
-                        for (int q = 0; q < NB; ++q) top = fmaxf(top, mw[q]);
-                        const float ms = top == -INFINITY ? 0.0f : top, f0 = exp2_(m - ms);
-                        m = top;
-                        l *= f0;
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) o[e] *= f0;
-#pragma unroll
-                        for (int q = 0; q < NB; ++q) {
-                            if (w + q > w1) continue;
-                            const float f = exp2_(mw[q] - ms);
-                            l = __builtin_fmaf(f, lw[q], l);
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) o[e] = __builtin_fmaf(f, ow[q][e], o[e]);
-                        }
-                    }
-                    put(r, d4, o, l);
+            const int n = w1 - w0 + 1;
+            int32_t *const heads_done = a.counters + (int64_t)s * heads + hk;
+            auto slot_of = [&](int w) { return w * 2 + (w == w0 ? 1 : 0); };
+            // Up to 16 partial results are joined by their last tile; more in two stages, 16 consecutive ones into a
+            // place (and with a counter) of the first one's, then those.
+            if (n <= kJoin) {
+                if (arrive(heads_done, n)) join(rows, n, [&](int i) { return slot_of(w0 + i); }, put);
+            } else {
+                const int first_tile = w0 + ((int)t - w0) / kJoin * kJoin, here = w1 - first_tile + 1 < kJoin ? w1 - first_tile + 1 : kJoin;
+                const int groups = (n + kJoin - 1) / kJoin, place = slot_of(first_tile), second = 2 * (int)a.T;
+                if (arrive(a.counters + (int64_t)seqs * heads + place, here)) {
+                    join(rows, here, [&](int i) { return slot_of(first_tile + i); }, [&](int r, int d4, const f32x4 &o, float m, float l) { keep(second + place, r, d4, o, m, l); });
+                    if (arrive(heads_done, groups)) join(rows, groups, [&](int i) { return second + slot_of(w0 + i * kJoin); }, put);
                 }
             }
         }
@@ -368,7 +404,7 @@ __global__ __launch_bounds__(kWave * P, DP > 128 ? 1 : 2) void attend_rows_kerne
         int base = 0, before = 0, mine = 0;  // first sequence of the 64, blocks before it, the lane's
         int upto = 0;                        // blocks up to and with the lane's sequence
         for (; base < seqs; base += kWave) {
-            mine = blocks_of(base + lane) * heads;
+            mine = list_of(base + lane) * heads;
             upto = mine;
 #pragma unroll
             for (int o = 1; o < kWave; o <<= 1) {
@@ -388,7 +424,8 @@ __global__ __launch_bounds__(kWave * P, DP > 128 ? 1 : 2) void attend_rows_kerne
                 while (hk < heads && at < stop) {
                     const int h0 = from + hk * nb, b0 = at - h0;
                     const int b1 = stop - h0 < nb ? stop - h0 : nb;
-                    run(t, base + i, hk, b0, b1, h0 / share, (h0 + nb - 1) / share);
+                    const int real = even ? blocks_of(base + i) : nb;  // (all places but perhaps the last)
+                    run(t, base + i, hk, b0, b1 < real ? b1 : real, h0 / share, (h0 + nb - 1) / share);
                     at = h0 + b1;
                     ++hk;
                 }
@@ -397,7 +434,7 @@ __global__ __launch_bounds__(kWave * P, DP > 128 ? 1 : 2) void attend_rows_kerne
                 before += __builtin_amdgcn_readlane(upto, kWave - 1);
                 base += kWave;
                 i = 0;
-                mine = blocks_of(base + lane) * heads;
+                mine = list_of(base + lane) * heads;
                 upto = mine;
 #pragma unroll
                 for (int o = 1; o < kWave; o <<= 1) {

@@ -217,7 +217,8 @@ static int create_attention(miriam_op *op) {
         outputs = d.seqs * d.kv_heads;
         if (outputs >= kMost || outputs > kMost / cdiv(keys, kRowKeys)) return einval("attention: too large for 32-bit block indexing");
         op->T = std::min<int64_t>(2 * cus, outputs * cdiv(keys, kRowKeys));
-        slots = 2 * op->T;
+        if (op->noalloc) op->T = std::min<int64_t>(op->T, (int64_t)(kScratchBytes - kScratchCounters) / (4 * part));
+        slots = 4 * op->T;  // two per tile, and as many for joining in two stages
         a.splits = (int32_t)std::min<int64_t>(op->T, 2);
     } else {
         // tiles of 128 query rows, their keys divided while there are fewer than two tiles per CU
@@ -236,8 +237,9 @@ static int create_attention(miriam_op *op) {
             op->T = outputs * a.splits;
             wbytes = op->T * part;
         }
-        // (the kernel for few rows: 8.6 MiB at most for head_dim up to 128, 16.9 MiB beyond)
-        const int wr = a.splits == 1 ? 0 : alloc_workspace(op, (size_t)wbytes, (size_t)(outputs * 4), false);
+        // counters of the outputs, and for few rows of the first stage of joining
+        const int64_t counters = outputs + (rows ? 2 * op->T : 0);
+        const int wr = a.splits == 1 ? 0 : alloc_workspace(op, (size_t)wbytes, (size_t)(counters * 4), false);
         if (wr < 0) return wr;
         if (wr == 0) {
             op->T = outputs;
