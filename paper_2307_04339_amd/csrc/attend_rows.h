@@ -59,13 +59,19 @@ __global__ __launch_bounds__(kWave * P, DP > 128 ? 1 : 2) void attend_rows_kerne
     const int64_t rank = wg_rank(blockIdx.x, G);
     const int seqs = (int)a.sq.seqs, heads = a.kv_heads, g = a.group;
 
-    // blocks of one cache head of sequence s; one where there are rows but no keys, to write their zeros
-    auto blocks_of = [&](int s) {
-        if (s >= seqs) return 0;
-        const SeqView v = seq_view(a, s);
-        if (v.n <= 0) return 0;
-        const int n = (v.end + kRowKeys - 1) / kRowKeys - v.begin / kRowKeys;
-        return n > 0 ? n : 1;
+    // 64 sequences from `base` on, one per lane: its view, the blocks of one of its cache heads (one where there are
+    // rows but no keys, to write their zeros), their places in the list, and the places up to and with them.
+    SeqView view;
+    int base = 0, blocks = 0, mine = 0, upto = 0;
+    auto look = [&](int from) {
+        base = from;
+        blocks = 0;
+        view = SeqView{};
+        if (base + lane < seqs) view = seq_view(a, base + lane);
+        if (view.n > 0) {
+            const int n = (view.end + kRowKeys - 1) / kRowKeys - view.begin / kRowKeys;
+            blocks = n > 0 ? n : 1;
+        }
     };
     // All blocks, and each tile's share.  While there are tiles enough for runs of two blocks that do not cross
     // from one head into the next, these are taken (a head's list then counts as even): two blocks take little
@@ -74,11 +80,10 @@ __global__ __launch_bounds__(kWave * P, DP > 128 ? 1 : 2) void attend_rows_kerne
     bool even = false;
     if (a.splits > 1) {
         int sum = 0, pairs = 0;
-#pragma unroll 4
-        for (int s = lane; s < seqs; s += kWave) {
-            const int n = blocks_of(s);
-            sum += n;
-            pairs += (n + 1) / 2;
+        for (int from = (seqs - 1) / kWave * kWave; from >= 0; from -= kWave) {  // (the first 64 stay)
+            look(from);
+            sum += blocks;
+            pairs += (blocks + 1) / 2;
         }
         for (int o = 32; o > 0; o >>= 1) {
             sum += __shfl_xor(sum, o);
@@ -90,9 +95,24 @@ __global__ __launch_bounds__(kWave * P, DP > 128 ? 1 : 2) void attend_rows_kerne
         if (even) total = 2 * pairs;
         share = even ? 2 : (total + (int)a.T - 1) / (int)a.T;
     }
-    auto list_of = [&](int s) {  // places of a head of sequence s in the list
-        const int n = blocks_of(s);
-        return even ? (n + 1) & ~1 : n;
+    auto list = [&]() {
+        mine = (even ? (blocks + 1) & ~1 : blocks) * heads;
+        upto = mine;
+#pragma unroll
+        for (int o = 1; o < kWave; o <<= 1) {
+            const int v = __shfl_up(upto, o);
+            upto += lane >= o ? v : 0;
+        }
+    };
+    auto view_of = [&](int i) {  // of the 64's i-th
+        SeqView v;
+        v.q0 = __builtin_amdgcn_readlane(view.q0, i);
+        v.n = __builtin_amdgcn_readlane(view.n, i);
+        v.pos0 = __builtin_amdgcn_readlane(view.pos0, i);
+        v.len = __builtin_amdgcn_readlane(view.len, i);
+        v.begin = __builtin_amdgcn_readlane(view.begin, i);
+        v.end = __builtin_amdgcn_readlane(view.end, i);
+        return v;
     };
 
     // A partial result into `slot` of the workspace, by device-coherent stores: another die's tile may join it.
@@ -156,8 +176,7 @@ __global__ __launch_bounds__(kWave * P, DP > 128 ? 1 : 2) void attend_rows_kerne
 
     // One run: blocks [b0, b1) of the nb of cache head hk of sequence s, the first of which is block `first`
     // of the sequence; tiles w0 .. w1 share the head.
-    auto run = [&](int64_t t, int s, int hk, int b0, int b1, int w0, int w1) __attribute__((always_inline)) {
-        const SeqView sv = seq_view(a, s);
+    auto run = [&](int64_t t, int s, const SeqView &sv, int hk, int b0, int b1, int w0, int w1) __attribute__((always_inline)) {
         const int rows = sv.n * g;
         const int first = sv.begin / kRowKeys;
         const T *const kh = KC + (int64_t)hk * a.sq.sh, *const vh = VC + (int64_t)hk * a.sq.sh;
@@ -393,54 +412,44 @@ __global__ __launch_bounds__(kWave * P, DP > 128 ? 1 : 2) void attend_rows_kerne
         if (a.splits <= 1) {
             // one tile per sequence and cache head
             const int s = (int)fdiv((uint32_t)t, a.fd_kv);
-            const int nb = blocks_of(s);
-            if (nb > 0) run(t, s, (int)t - s * heads, 0, nb, 0, 0);
+            look(s / kWave * kWave);
+            const int nb = __builtin_amdgcn_readlane(blocks, s % kWave);
+            if (nb > 0) run(t, s, view_of(s % kWave), (int)t - s * heads, 0, nb, 0, 0);
             continue;
         }
         int at = (int)t * share;
         const int stop = at + share < total ? at + share : total;
         if (at >= stop) continue;
-        // the sequence of block `at`: 64 at a time
-        int base = 0, before = 0, mine = 0;  // first sequence of the 64, blocks before it, the lane's
-        int upto = 0;                        // blocks up to and with the lane's sequence
-        for (; base < seqs; base += kWave) {
-            mine = list_of(base + lane) * heads;
-            upto = mine;
-#pragma unroll
-            for (int o = 1; o < kWave; o <<= 1) {
-                const int v = __shfl_up(upto, o);
-                upto += lane >= o ? v : 0;
-            }
+        // the sequence of place `at`
+        if (base != 0) look(0);
+        int before = 0;  // places before the 64
+        for (list(); base < seqs; list()) {
             const int all = __builtin_amdgcn_readlane(upto, kWave - 1);
             if (before + all > at) break;
             before += all;
+            look(base + kWave);
         }
         int i = __builtin_popcountll(__ballot(before + upto <= at));
         while (at < stop && base < seqs) {
             const int nbs = __builtin_amdgcn_readlane(mine, i);
             if (nbs > 0) {
                 const int from = before + __builtin_amdgcn_readlane(upto, i) - nbs, nb = nbs / heads;
+                const int real = __builtin_amdgcn_readlane(blocks, i);  // (all places but perhaps the last)
+                const SeqView sv = view_of(i);
                 int hk = (at - from) / nb;
                 while (hk < heads && at < stop) {
                     const int h0 = from + hk * nb, b0 = at - h0;
                     const int b1 = stop - h0 < nb ? stop - h0 : nb;
-                    const int real = even ? blocks_of(base + i) : nb;  // (all places but perhaps the last)
-                    run(t, base + i, hk, b0, b1 < real ? b1 : real, h0 / share, (h0 + nb - 1) / share);
+                    run(t, base + i, sv, hk, b0, b1 < real ? b1 : real, h0 / share, (h0 + nb - 1) / share);
                     at = h0 + b1;
                     ++hk;
                 }
             }
             if (++i >= kWave && at < stop) {
                 before += __builtin_amdgcn_readlane(upto, kWave - 1);
-                base += kWave;
                 i = 0;
-                mine = list_of(base + lane) * heads;
-                upto = mine;
-#pragma unroll
-                for (int o = 1; o < kWave; o <<= 1) {
-                    const int v = __shfl_up(upto, o);
-                    upto += lane >= o ? v : 0;
-                }
+                look(base + kWave);
+                list();
             }
         }
     }
