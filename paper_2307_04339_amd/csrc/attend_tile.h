@@ -10,9 +10,22 @@
 // Where a load's rows (4 of 256 bytes) always lie in one page, its base is scalar and the lanes' offsets never
 // change (UNI); otherwise every lane finds its row by itself.
 //
-// Tiles of one cache head are consecutive, so a die's tiles share its L2's keys, and run from a sequence's last
-// rows to its first: the longest first.  With fewer than two tiles per CU a tile's keys are divided among
-// `splits` tiles, the last of which joins their partial results in order.
+// Row tiles of one cache head are consecutive, so a die's tiles share its L2's keys, and run from a sequence's
+// last rows to its first: the longest first.  Every tile finds out by itself how the batch, as it is on the device,
+// is divided (some microseconds, with row tiles across the lanes):
+//  - Many row tiles, none of them longer than twice what each of the 2 x CUs workgroups that run at once gets:
+//    a tile each, as the hardware hands them out.
+//  - Fewer row tiles than such workgroups, of like lengths (a chunk behind a long context): every row tile is cut
+//    into about equal pieces, at the same keys for all row tiles of a sequence, which then share them in L2
+//    (512 tokens behind 16k: 178 us, in equal runs of the list below 205).
+//  - Otherwise (single tokens beside chunks): the steps of all row tiles form a list of which every tile takes an
+//    equal run (20 sequences of 1 to 400 tokens: 61 us, in pieces 70, a fixed division of every row tile 86).  As
+//    a second row tile's start and the joining cost more than a few steps, a run's end that lies within a third of
+//    a run of a row tile's is moved there.
+// A row tile that ends up in several tiles is joined by the last of them to arrive, in their order.
+//
+// 4 prompts of 4096 tokens, 32 heads of 128: 690 to 715 us, 770 to 800 TFLOP/s of the products that are needed.  The
+// matrix instructions and their operands' reads from LDS alone take 485 us, the powers of two another 110.
 #pragma once
 
 #include "attend.h"
@@ -30,6 +43,7 @@ struct TileKernel {
     static constexpr int HALF = kTileKeys * DP * 2;  // a stage of keys or of values
     static constexpr int LDS_BYTES = 4 * HALF;
     static constexpr int NI = NLD / P;        // loads of a wave
+    static constexpr int PARTS = LDS_BYTES / (kTileRows * 8);  // partial results that can be joined
     // loads q of a wave whose rows are swizzled differently: q mod 4 (DP = 128), 2 (64), 8 (256)
     static constexpr int CYC = DP == 64 ? 2 : DP == 128 ? 4 : 8, NSW = CYC / P > 0 ? CYC / P : 1;
     // pieces are exchanged so that what a read takes from several rows lies on different banks
@@ -68,63 +82,277 @@ __global__ __launch_bounds__(kWave * P, DP > 128 ? 1 : 2) void attend_tile_kerne
     const int64_t G = gridDim.x;
     const int64_t rank = wg_rank(blockIdx.x, G);
     const int seqs = (int)a.sq.seqs, g = a.group;
-    const int outputs = (int)(a.T / a.splits), per_head = outputs / a.kv_heads;
+
+    // 64 sequences from `base` on, one per lane, and their row tiles
+    SeqView view;
+    int base = -1, ntiles = 0;
+    auto look = [&](int from) {
+        if (from == base) return;
+        base = from;
+        view = SeqView{};
+        if (base + lane < seqs) view = seq_view(a, base + lane);
+        ntiles = (view.n * g + kTileRows - 1) / kTileRows;
+    };
+    auto at_lane = [&](const SeqView &of, int i) {
+        SeqView v;
+        v.q0 = __builtin_amdgcn_readlane(of.q0, i);
+        v.n = __builtin_amdgcn_readlane(of.n, i);
+        v.pos0 = __builtin_amdgcn_readlane(of.pos0, i);
+        v.len = __builtin_amdgcn_readlane(of.len, i);
+        v.begin = v.end = 0;
+        return v;
+    };
+    // keys that the rows of row tile q may see, and the positions of its first and last row
+    struct Span {
+        int begin, end, lo, hi;
+    };
+    auto span = [&](const SeqView &v, int q) {
+        const int row0 = q * kTileRows, last = v.n * g < row0 + kTileRows ? v.n * g - 1 : row0 + kTileRows - 1;
+        Span p;
+        p.lo = v.pos0 + (int)fdiv((uint32_t)row0, a.fd_group);
+        p.hi = v.pos0 + (int)fdiv((uint32_t)last, a.fd_group);
+        p.end = a.causal ? clampi(p.hi + 1, 0, v.len) : v.len;
+        p.begin = a.window > 0 ? clampi(p.lo - a.window + 1, 0, p.end) : 0;
+        return p;
+    };
+    auto steps = [&](const Span &p) {  // one where there are no keys, to write the rows' zeros
+        return p.end > p.begin ? (p.end + kTileKeys - 1) / kTileKeys - p.begin / kTileKeys : 1;
+    };
+    auto scan = [&](int n) {
+#pragma unroll
+        for (int o = 1; o < kWave; o <<= 1) {
+            const int v = __shfl_up(n, o);
+            n += lane >= o ? v : 0;
+        }
+        return n;
+    };
+    // row tiles 64 c .. 64 c + 63 of a cache head, one per lane: whose, which of its, and its steps (0: none)
+    struct Chunk {
+        int s, qi, n;
+        SeqView v;
+    };
+    auto chunk = [&](int c) {
+        Chunk r = {};
+        const int want = c * kWave + lane;
+        for (int from = 0, before = 0; from < seqs; from += kWave) {
+            look(from);
+            const int upto = scan(ntiles), all = __builtin_amdgcn_readlane(upto, kWave - 1);
+            int i = 0;  // sequences of these that end at or before it
+#pragma unroll
+            for (int o = kWave / 2; o > 0; o >>= 1) i += __shfl(upto, i + o - 1) <= want - before ? o : 0;
+            SeqView v = view;
+            v.q0 = __shfl(view.q0, i);
+            v.n = __shfl(view.n, i);
+            v.pos0 = __shfl(view.pos0, i);
+            v.len = __shfl(view.len, i);
+            const int end = __shfl(upto, i);
+            if (want >= before && want - before < all) {
+                r.s = from + i;
+                r.qi = end - 1 - (want - before);  // a sequence's last rows first
+                r.v = v;
+                r.n = steps(span(v, r.qi));
+            }
+            before += all;
+            if (before > c * kWave + kWave - 1) break;
+        }
+        return r;
+    };
+    // row tiles of a cache head, the longest sequence's steps, and at least half of all
+    int J = 0, longest = 0;
+    float half = 0.0f;
+    for (int from = (seqs - 1) / kWave * kWave; from >= 0; from -= kWave) {  // (the first 64 stay)
+        look(from);
+        int k = ntiles, n = ntiles > 0 && view.end > view.begin ? (view.end + kTileKeys - 1) / kTileKeys - view.begin / kTileKeys : 0;
+        float h = 0.5f * (float)n * (float)ntiles;
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) {
+            const int v = __shfl_xor(n, o);
+            n = v > n ? v : n;
+            k += __shfl_xor(k, o);
+            h += __shfl_xor(h, o);
+        }
+        J += k;
+        longest = longest > n ? longest : n;
+        half += h;
+    }
+    J = __builtin_amdgcn_readfirstlane(J);
+    longest = __builtin_amdgcn_readfirstlane(longest);
+    const bool many = J * a.kv_heads >= 4 * a.runs && (float)longest * (float)a.runs <= 2.0f * half * (float)a.kv_heads;
+    // (more row tiles than rows can have: starts that overlap; no tile may then wait for another's part)
+    const bool list = a.splits > 1 && J <= a.tiles && !__builtin_amdgcn_readfirstlane(many);
+    if (J > a.tiles) J = a.tiles;
+    // Places of the list: a row tile's steps, or with unit > 0 its pieces of about `unit` steps.  Of a cache head,
+    // and of tile k: [start(k), start(k + 1))
+    int unit = 0, head_places = 0, runs = 1, near = 1;
+    auto places = [&](int n) { return unit == 0 || n == 0 ? n : n < unit ? 1 : (n + unit / 2) / unit; };
+    const int chunks = (J + kWave - 1) / kWave;
+    Chunk ch = {};
+    int have = -1;
+    auto get = [&](int c) {
+        if (c != have) ch = chunk(have = c);
+    };
+    int biggest = 0;  // piece
+    auto count = [&]() {
+        head_places = biggest = 0;
+        for (int c = chunks - 1; c >= 0; --c) {
+            get(c);
+            int n = places(ch.n), m = n > 0 ? (ch.n + n - 1) / n : 0;
+#pragma unroll
+            for (int o = 32; o > 0; o >>= 1) {
+                const int v = __shfl_xor(m, o);
+                m = v > m ? v : m;
+                n += __shfl_xor(n, o);
+            }
+            head_places += __builtin_amdgcn_readfirstlane(n);
+            m = __builtin_amdgcn_readfirstlane(m);
+            biggest = biggest > m ? biggest : m;
+        }
+    };
+    if (list) {
+        // runs and pieces of four steps at least, and as many as the parts of a row tile that can be joined need
+        const int room = (longest + K_::PARTS - 3) / (K_::PARTS - 2), least = room > 4 ? room : 4;
+        count();
+        const int all = head_places * a.kv_heads, each = all / a.runs;
+        if (J * a.kv_heads <= a.runs) {
+            unit = each > least ? each : least;
+            count();
+            // (fewer pieces than there are workgroups to take them, of equal lengths)
+            if (head_places * a.kv_heads > a.runs || 4 * biggest > 5 * unit) unit = 0;
+            runs = head_places * a.kv_heads;
+        }
+        if (unit == 0) {
+            head_places = all / a.kv_heads;
+            runs = all / least;
+            runs = runs < 1 ? 1 : runs < a.runs ? runs : a.runs;
+            near = all / runs / 3;
+            near = near > 1 ? near : 1;
+        }
+    }
+    const int total = head_places * a.kv_heads, run = total / runs, more = total - run * runs;
+    auto start = [&](int k) { return k * run + k * more / runs; };  // floor(k total / runs)
 
     int iter = 0;
     for (int64_t t = sh.begin + rank; t < sh.begin + sh.len; t += G, ++iter) {
         trace_tile(sh, t, iter);
         for (int slot = 0; slot < kLogicalWaves / P; ++slot) trace_wave(sh, t, slot * P + pw, pw, slot);
-        const int out = (int)fdiv((uint32_t)t, a.fd_splits), split = (int)t - out * a.splits;
-        const int hk = out / per_head;
-        int qi = out - hk * per_head;
-        // the qi-th of all sequences' row tiles
-        int s = -1;
-        for (int base = 0; base < seqs; base += kWave) {
-            int n = 0;
-            if (base + lane < seqs) n = (seq_view(a, base + lane).n * g + kTileRows - 1) / kTileRows;
-            int upto = n;
-#pragma unroll
-            for (int o = 1; o < kWave; o <<= 1) {
-                const int v = __shfl_up(upto, o);
-                upto += lane >= o ? v : 0;
-            }
-            const int all = __builtin_amdgcn_readlane(upto, kWave - 1);
-            if (qi < all) {
-                const int i = __builtin_popcountll(__ballot(upto <= qi));
-                s = base + i;
-                qi = __builtin_amdgcn_readlane(upto, i) - 1 - qi;  // a sequence's last rows first
-                break;
-            }
-            qi -= all;
+        // ---- where the tile begins: row tile j of cache head hk, which is row tile qi of sequence s; in the list
+        // place `inside` of it, and place `at` of all
+        int at = 0, stop = 1, hk, j, s = -1, qi = 0, inside = 0;
+        if (list) {
+            if (t >= runs) continue;
+            at = start((int)t);
+            stop = start((int)t + 1);
+            hk = at / head_places;
+            inside = at - hk * head_places;
+            j = 0;
+        } else {
+            if (t >= (int64_t)J * a.kv_heads) continue;
+            hk = (int)t / J;
+            j = (int)t - hk * J;
         }
+        SeqView sv;
+        if (list) {
+            for (int c = 0; c < chunks && s < 0; ++c) {
+                get(c);
+                const int upto = scan(places(ch.n)), here = __builtin_amdgcn_readlane(upto, kWave - 1);
+                if (inside < here) {
+                    const int i = __builtin_popcountll(__ballot(upto <= inside));
+                    inside -= i > 0 ? __builtin_amdgcn_readlane(upto, i - 1) : 0;
+                    j = c * kWave + i;
+                    s = __builtin_amdgcn_readlane(ch.s, i);
+                    qi = __builtin_amdgcn_readlane(ch.qi, i);
+                    sv = at_lane(ch.v, i);
+                } else {
+                    inside -= here;
+                }
+            }
+        } else {
+            for (int from = 0, before = 0; from < seqs && s < 0; from += kWave) {
+                look(from);
+                const int upto = scan(ntiles), all = __builtin_amdgcn_readlane(upto, kWave - 1);
+                if (j - before < all) {
+                    const int i = __builtin_popcountll(__ballot(upto <= j - before));
+                    s = from + i;
+                    qi = __builtin_amdgcn_readlane(upto, i) - 1 - (j - before);
+                    sv = at_lane(view, i);
+                }
+                before += all;
+            }
+        }
+        // (what the next tile looks up anew: it is not to hold registers through this one's work)
+        ch = Chunk{};
+        view = SeqView{};
+        ntiles = 0;
+        have = base = -1;
         if (s < 0) continue;
-        const SeqView sv = seq_view(a, s);
-        const int row0 = qi * kTileRows, rows = sv.n * g - row0 < kTileRows ? sv.n * g - row0 : kTileRows;
-        // keys that the tile's rows may see, in steps of 64, and this split's share
-        SeqView tv = sv;
-        int tile_lo, tile_hi;  // positions of the tile's first and last row
-        {
-            const int t0 = (int)fdiv((uint32_t)row0, a.fd_group), t1 = (int)fdiv((uint32_t)(row0 + rows - 1), a.fd_group);
-            tile_lo = sv.pos0 + t0;
-            tile_hi = sv.pos0 + t1;
-            tv.end = a.causal ? clampi(sv.pos0 + t1 + 1, 0, sv.len) : sv.len;
-            tv.begin = a.window > 0 ? clampi(sv.pos0 + t0 - a.window + 1, 0, tv.end) : 0;
+        // ---- its pieces of row tiles, one after another.  A run ends inside a row tile only if that leaves `near`
+        // steps or more on both sides; nearer ends are moved to the row tile's.
+        auto onward = [&]() {  // to the next row tile of the list
+            inside = 0;
+            ++j;
+            if (--qi < 0) {
+                do {
+                    if (++s == seqs) {
+                        s = 0;
+                        j = 0;
+                        ++hk;
+                    }
+                    sv = seq_view(a, s);
+                } while (sv.n <= 0 && hk < a.kv_heads);
+                qi = (sv.n * g + kTileRows - 1) / kTileRows - 1;
+            }
+        };
+        if (list && unit == 0 && inside > 0) {
+            const int nb = steps(span(sv, qi));
+            if (inside < near) {
+                at -= inside;
+                inside = 0;
+            } else if (nb - inside < near) {
+                at += nb - inside;
+                onward();
+            }
         }
-        const int lo = tv.begin / kTileKeys, nb = tv.end > tv.begin ? (tv.end + kTileKeys - 1) / kTileKeys - lo : 0;
-        const int b0 = lo + (int)((int64_t)split * nb / a.splits), b1 = lo + (int)((int64_t)(split + 1) * nb / a.splits);
+        while (at < stop && hk < a.kv_heads && j < J) {
+        const Span tv = span(sv, qi);
+        const int tile_lo = tv.lo, tile_hi = tv.hi;
+        const int row0 = qi * kTileRows, rows = sv.n * g - row0 < kTileRows ? sv.n * g - row0 : kTileRows;
+        const int lo = tv.begin / kTileKeys, nb = steps(tv), out = hk * J + j;
+        int skip = inside, take = nb - inside, w0 = (int)t, w1 = (int)t;  // steps of this piece; the tiles that share the row tile
+        if (list && unit > 0) {
+            const int n = places(nb);
+            skip = (int)((int64_t)nb * inside / n);
+            take = (int)((int64_t)nb * (inside + 1) / n) - skip;
+            w0 = (int)t - inside;
+            w1 = w0 + n - 1;
+        } else if (list) {
+            const int h0 = at - inside, e = stop - h0;  // where the row tile begins, and the run ends in it
+            if (e < nb && e < near) break;
+            if (e < nb && nb - e >= near) take = e - inside;
+            // the runs that share it: those around the starts that lie in it; start(k) >= v from k = ceil(v runs / total) on
+            auto from = [&](int v) { return (int)(((int64_t)v * runs + total - 1) / total); };
+            const int k0 = from(h0 + near), k1 = from(h0 + nb - near + 1) - 1;
+            if (nb >= 2 * near && k1 >= k0) {
+                w0 = k0 - 1;
+                w1 = k1;
+            }
+        }
+        const int b0 = lo + skip, b1 = tv.end > tv.begin ? b0 + take : b0;
+        auto slot_at = [&](int w) { return (uint32_t)(2 * w + (w == w0 ? 1 : 0)) * (uint32_t)(attend_partial(kTileRows, DP) * 4); };  // run w's partial result
         const T *const kh = static_cast<const T *>(a.k) + (int64_t)hk * a.sq.sh, *const vh = static_cast<const T *>(a.v) + (int64_t)hk * a.sq.sh;
 
         // Page-table entries of a step: UNI: of its load (lane mod NLD), else of the lane's rows and of key `lane`.
         constexpr int NE = UNI ? 1 : K_::NI + 1;
-        int32_t id[NE], slot_of[NE];
-        auto fetch = [&](int b) {
+        struct Entry {
+            int32_t id[NE], slot[NE];
+        };
+        auto fetch = [&](int b, Entry &n) {
             auto entry = [&](int j, int i) {
-                id[i] = -1;
-                slot_of[i] = 0;
+                n.id[i] = -1;
+                n.slot[i] = 0;
                 if (b < b1 && j < tv.end && (UNI ? j + RPL > tv.begin : j >= tv.begin)) {
                     const int pg = (int)fdiv((uint32_t)j, a.sq.fd_page);
-                    slot_of[i] = j - pg * a.sq.page;
-                    if (pg < a.sq.max_pages) id[i] = a.sq.table[s * a.sq.ldt + pg];
+                    n.slot[i] = j - pg * a.sq.page;
+                    if (pg < a.sq.max_pages) n.id[i] = a.sq.table[s * a.sq.ldt + pg];
                 }
             };
             if constexpr (UNI) {
@@ -140,12 +368,12 @@ __global__ __launch_bounds__(kWave * P, DP > 128 ? 1 : 2) void attend_tile_kerne
             int64_t off[UNI ? 1 : K_::NI];
             uint64_t there;
         };
-        auto resolve = [&](int b) {
+        auto resolve = [&](int b, const Entry &n) {
             Where w;
 #pragma unroll
             for (int i = 0; i < (UNI ? 1 : K_::NI); ++i) {
-                const bool ok = id[i] >= 0 && id[i] < a.sq.pages;
-                w.off[i] = ok ? (id[i] * a.sq.sp + (int64_t)slot_of[i] * a.sq.st) * 2 : -1;
+                const bool ok = n.id[i] >= 0 && n.id[i] < a.sq.pages;
+                w.off[i] = ok ? (n.id[i] * a.sq.sp + (int64_t)n.slot[i] * a.sq.st) * 2 : -1;
             }
             if constexpr (UNI) {
                 const uint64_t groups = __ballot(w.off[0] >= 0);
@@ -156,7 +384,7 @@ __global__ __launch_bounds__(kWave * P, DP > 128 ? 1 : 2) void attend_tile_kerne
                     w.there = __ballot(((groups >> (lane / RPL)) & 1) && j >= tv.begin && j < tv.end);
                 }
             } else {
-                w.there = __ballot(id[K_::NI] >= 0 && id[K_::NI] < a.sq.pages);
+                w.there = __ballot(n.id[K_::NI] >= 0 && n.id[K_::NI] < a.sq.pages);
             }
             return w;
         };
@@ -358,16 +586,17 @@ __global__ __launch_bounds__(kWave * P, DP > 128 ? 1 : 2) void attend_tile_kerne
 
             if (b0 < b1) {
                 Scores za, zb;
+                Entry e, e1;
+                fetch(b0, e);
+                fetch(b0 + 1, e1);
+                Where w0 = resolve(b0, e), wn = resolve(b0 + 1, e1);
+                uint64_t here = w0.there;  // keys of the step that are there
                 __syncthreads();  // the previous round's stages are free
-                fetch(b0);
-                Where w0 = resolve(b0);
-                fetch(b0 + 1);
                 load(b0, w0, kh, ko, lds0 + stage(0));
                 load(b0, w0, vh, vo, lds0 + stage(2));
-                uint64_t here = w0.there;  // keys of the step that are there
-                w0 = resolve(b0 + 1);
-                fetch(b0 + 2);
+                w0 = wn;
                 if (b0 + 1 < b1) load(b0 + 1, w0, kh, ko, lds0 + stage(1));
+                fetch(b0 + 2, e);
                 wait_vmcnt<0>();
                 __syncthreads();
                 first(b0, za, here);
@@ -378,10 +607,10 @@ __global__ __launch_bounds__(kWave * P, DP > 128 ? 1 : 2) void attend_tile_kerne
                     // loads to come overwrite
                     wait_vmcnt<0>();
                     __syncthreads();
-                    const Where w1 = resolve(b + 2);
+                    const Where w1 = resolve(b + 2, e);
                     if (b + 2 < b1) load(b + 2, w1, kh, ko, lds0 + stage(odd));
                     if (b + 1 < b1) load(b + 1, w0, vh, vo, lds0 + stage(2 + (odd ^ 1)));
-                    fetch(b + 3);
+                    fetch(b + 3, e);
                     const int kb = b * kTileKeys;
                     // (the same for all waves: what the tile's first and last rows do not all see)
                     if ((a.causal && kb + kTileKeys - 1 > tile_lo) || (a.window > 0 && kb <= tile_hi - a.window)) take_apart(kb, 2 + odd, here);
@@ -402,7 +631,7 @@ __global__ __launch_bounds__(kWave * P, DP > 128 ? 1 : 2) void attend_tile_kerne
                 const auto s32 = __builtin_amdgcn_permlane32_swap(u, u, false, false);
                 l = __builtin_bit_cast(float, (uint32_t)s32[0]) + __builtin_bit_cast(float, (uint32_t)s32[1]);
                 if (xl >= wrows) {
-                } else if (a.splits <= 1) {
+                } else if (w0 == w1) {
                     const float inv = l > 0.0f || l != l ? 1.0f / l : 0.0f;  // no key: zeros
                     T *yr = Y + (int64_t)(sv.q0 + tok) * a.ldy + (int64_t)(hk * g + r - tok * g) * a.d;
 #pragma unroll
@@ -418,7 +647,7 @@ __global__ __launch_bounds__(kWave * P, DP > 128 ? 1 : 2) void attend_tile_kerne
                         }
                 } else {
                     // partial result as the lanes hold it, device-coherent: another die's tile may join it
-                    const uint32_t at = (uint32_t)t * (uint32_t)(attend_partial(kTileRows, DP) * 4), pr = (uint32_t)(32 * lam + xl);
+                    const uint32_t at = slot_at((int)t), pr = (uint32_t)(32 * lam + xl);
 #pragma unroll
                     for (int i = 0; i < ND; ++i)
 #pragma unroll
@@ -434,55 +663,57 @@ __global__ __launch_bounds__(kWave * P, DP > 128 ? 1 : 2) void attend_tile_kerne
                 }
             }
         }
-        if (a.splits > 1) {
+        if (w0 != w1) {
             // the partial result's stores complete before the arrival is counted
+            const int parts = w1 - w0 + 1;
             __builtin_amdgcn_s_waitcnt(0);
             __syncthreads();
             if (tid == 0) {
                 const int prev = __hip_atomic_fetch_add(a.counters + out, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-                s_last = prev == a.splits - 1;
+                s_last = prev == parts - 1;
                 if (s_last) __hip_atomic_store(a.counters + out, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
             }
             __syncthreads();
             if (s_last) {
-                // each split's share of each row's sum, in LDS (the stages are free); then the outputs, the loads of
-                // several of a thread in flight
-                float *const weight = reinterpret_cast<float *>(smem);  // [splits][kTileRows]
-                const uint32_t part = (uint32_t)(attend_partial(kTileRows, DP) * 4), at0 = (uint32_t)out * (uint32_t)a.splits * part;
-                auto word = [&](int w, uint32_t i) {
-                    return __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rw, (int)(at0 + (uint32_t)w * part + i * 4u), 0, kAgent));
-                };
+                // each part's maxima and sums, then its share of each row's sum, in LDS (the stages are free); then
+                // the outputs, the loads of several pieces in flight
+                float *const weight = reinterpret_cast<float *>(smem), *const sums = weight + K_::PARTS * kTileRows;  // [parts][kTileRows]
+#pragma unroll 8
+                for (int i = tid; i < parts * kTileRows; i += kWave * P) {
+                    const int w = i / kTileRows, r = i % kTileRows;
+                    const uint32_t from = slot_at(w0 + w) + (uint32_t)(kTileRows * DP + r) * 4u;
+                    weight[i] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rw, (int)from, 0, kAgent));
+                    sums[i] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rw, (int)(from + kTileRows * 4u), 0, kAgent));
+                }
+                __syncthreads();
                 for (int r = tid; r < rows; r += kWave * P) {
-                    float top = -INFINITY, sum = 0.0f;
-                    for (int w = 0; w < a.splits; ++w) {
-                        const float mw = word(w, (uint32_t)(kTileRows * DP + r));
-                        weight[w * kTileRows + r] = mw;
-                        top = fmaxf(top, mw);
-                    }
+                    float top = -INFINITY, all = 0.0f;
+                    for (int w = 0; w < parts; ++w) top = fmaxf(top, weight[w * kTileRows + r]);
                     const float ms = top == -INFINITY ? 0.0f : top;
-                    for (int w = 0; w < a.splits; ++w) {
+                    for (int w = 0; w < parts; ++w) {
                         const float f = exp2_(weight[w * kTileRows + r] - ms);
                         weight[w * kTileRows + r] = f;
-                        sum = __builtin_fmaf(f, word(w, (uint32_t)(kTileRows * (DP + 1) + r)), sum);
+                        all = __builtin_fmaf(f, sums[w * kTileRows + r], all);
                     }
-                    const float inv = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
-                    for (int w = 0; w < a.splits; ++w) weight[w * kTileRows + r] *= inv;
+                    const float inv = all > 0.0f || all != all ? 1.0f / all : 0.0f;
+                    for (int w = 0; w < parts; ++w) weight[w * kTileRows + r] *= inv;
                 }
                 __syncthreads();
                 // piece i of a partial result: values 32 (i / 256 % ND) + 8 (i / 64 % 4) + 4 (i / 32 % 2) .. of row
                 // 32 (i / (256 ND)) + i % 32
-                constexpr int PIECES = kTileRows * DP / 4, step = kWave * P, NB = 8;
-                for (int i0 = tid; i0 < PIECES; i0 += NB * step) {
+                constexpr int step = kWave * P, NB = 8;
+                for (int i0 = tid; i0 < (rows + 31) / 32 * (256 * ND); i0 += NB * step) {
                     f32x4 o[NB];
 #pragma unroll
                     for (int j = 0; j < NB; ++j) o[j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
                     auto row_of = [&](int j) { return 32 * ((i0 + j * step) / (256 * ND)) + (i0 + j * step) % 32; };
                     auto col_of = [&](int j) { return 32 * ((i0 + j * step) / 256 % ND) + 8 * ((i0 + j * step) / 64 % 4) + 4 * ((i0 + j * step) / 32 % 2); };
-                    for (int w = 0; w < a.splits; ++w) {
+#pragma unroll 2
+                    for (int w = 0; w < parts; ++w) {
                         f32x4 ow[NB];
 #pragma unroll
                         for (int j = 0; j < NB; ++j)  // (rows and values that are not there lie in the workspace, too)
-                            ow[j] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(rw, (int)(at0 + (uint32_t)w * part + (uint32_t)(i0 + j * step) * 16u), 0, kAgent));
+                            ow[j] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(rw, (int)(slot_at(w0 + w) + (uint32_t)(i0 + j * step) * 16u), 0, kAgent));
 #pragma unroll
                         for (int j = 0; j < NB; ++j) {
                             const float f = weight[w * kTileRows + row_of(j)];
@@ -504,6 +735,9 @@ __global__ __launch_bounds__(kWave * P, DP > 128 ? 1 : 2) void attend_tile_kerne
                 }
             }
             __syncthreads();  // s_last is free
+        }
+        at += list && unit == 0 ? take : 1;
+        if (at < stop) onward();
         }
     }
 }

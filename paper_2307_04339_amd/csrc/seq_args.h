@@ -53,11 +53,12 @@ struct AttendArgs {
     SeqArgs sq;
     int64_t ldx, ldy;
     int32_t heads, kv_heads, group, d;  // group = query heads per cache head
-    FastDiv fd_group, fd_kv, fd_splits; // division by group, kv_heads and splits
+    FastDiv fd_group, fd_kv;  // division by group and kv_heads
     int32_t max_q, window, causal;
     float scale;              // times log2(e): the exponentials are powers of two
-    int32_t splits;           // 1: every output is finished by one tile
+    int32_t splits;           // 1: every output is finished by one tile, 2: tiles may share one
     int64_t T;
+    int32_t runs, tiles;      // many rows: tiles that share the list of all steps; row tiles of a cache head, at most
     float *work;              // partial results
     uint32_t work_bytes;
     int32_t *counters;        // arrivals per output; back to 0 once a pass over the op completes

@@ -221,28 +221,27 @@ static int create_attention(miriam_op *op) {
         slots = 4 * op->T;  // two per tile, and as many for joining in two stages
         a.splits = (int32_t)std::min<int64_t>(op->T, 2);
     } else {
-        // tiles of 128 query rows, their keys divided while there are fewer than two tiles per CU
+        // a tile for every 128 query rows that there may be, and two per CU at least, which share the steps of a
+        // smaller batch
+        if (keys >= (int64_t)1 << 26) return einval("attention: page * max_pages must be below 2^26 for more than 16 query rows per cache head");
         const int64_t qt = std::min(d.tokens * a.group / kTileRows + d.seqs, d.seqs * cdiv((int64_t)a.max_q * a.group, kTileRows));
         if (qt >= kMost / d.kv_heads) return einval("attention: too large for 32-bit tile indexing");
         outputs = qt * d.kv_heads;
-        a.splits = (int32_t)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(2 * cus / outputs, 64), cdiv(keys, 4 * kTileKeys)));
-        op->T = outputs * a.splits;
-        slots = op->T;
+        a.tiles = (int32_t)qt;
+        // (as many as runs of four steps of full caches, and in the device scratch as have room)
+        int64_t runs = std::min<int64_t>(2 * cus, cdiv(outputs * cdiv(keys, kTileKeys), 4));
+        if (op->noalloc) runs = std::min<int64_t>(runs, (int64_t)(kScratchBytes - kScratchCounters) / (2 * part));
+        a.runs = (int32_t)runs;
+        op->T = std::max(outputs, runs);
+        slots = 2 * runs;
+        a.splits = runs > 1 && cdiv(keys, kTileKeys) > 4 ? 2 : 1;
     }
     if (a.splits > 1) {
-        int64_t wbytes = slots * part;
-        const int64_t room = op->noalloc ? (int64_t)(kScratchBytes - kScratchCounters) : (int64_t)1 << 30;
-        if (wbytes > room && !rows) {
-            a.splits = (int32_t)std::max<int64_t>(1, room / (outputs * part));
-            op->T = outputs * a.splits;
-            wbytes = op->T * part;
-        }
         // counters of the outputs, and for few rows of the first stage of joining
-        const int64_t counters = outputs + (rows ? 2 * op->T : 0);
-        const int wr = a.splits == 1 ? 0 : alloc_workspace(op, (size_t)wbytes, (size_t)(counters * 4), false);
+        const int64_t wbytes = slots * part, counters = outputs + (rows ? 2 * op->T : 0);
+        const int wr = alloc_workspace(op, (size_t)wbytes, (size_t)(counters * 4), false);
         if (wr < 0) return wr;
         if (wr == 0) {
-            op->T = outputs;
             a.splits = 1;
         } else {
             a.work = static_cast<float *>(op->work);
@@ -250,8 +249,8 @@ static int create_attention(miriam_op *op) {
             a.counters = static_cast<int32_t *>(op->counters);
         }
     }
+    if (a.splits == 1) op->T = outputs;
     if (op->T >= (int64_t)INT32_MAX) return einval("attention: too large for 32-bit tile indexing");
-    a.fd_splits = make_fastdiv((uint32_t)a.splits);
     a.T = op->T;
     // many rows: the rows of one load (512 / dp keys) always in one page
     const bool f16 = d.dtype == MIRIAM_F16, uni = d.page % (512 / dp) == 0 && d.cache_token < ((int64_t)1 << 26);

@@ -282,6 +282,39 @@ def test_attention_over_long_caches(ops, seq, orc, dtype, new, ctx):
     elastic_bitwise(op, [y], orc, bits)
 
 
+DIVISIONS = [
+    # new, ctx, heads, kv_heads, d, page, token_major, window, max_q: how the work is divided among tiles
+    ([20] * 70, [20 + 37 * i % 900 for i in range(70)], 8, 8, 64, 16, False, 0, None),     # more row tiles than run at once
+    ([130] * 9 + [1], [130 + 50 * i for i in range(9)] + [30000], 64, 32, 64, 32, False, 0, None),  # one very long sequence beside them
+    ([1, 300, 1, 77, 1, 1], [3000, 700, 50, 4000, 1, 2047], 10, 5, 128, 24, True, 1500, None),  # single tokens beside chunks
+    ([513], [9000], 4, 1, 128, 16, False, 0, None),                                        # one chunk, one cache head
+    ([40, 3], [40, 60000], 2, 1, 64, 64, False, 0, None),                                  # as many parts as can be joined
+    ([2100], [2100], 32, 32, 64, 64, False, 0, None),                                      # a tile for each
+    ([1] * 200, [1 + 11 * i % 700 for i in range(200)], 8, 4, 64, 16, False, 0, 1),        # single tokens of many sequences
+    ([1, 1, 1], [40000, 3, 129], 2, 1, 128, 64, False, 0, 1),                              # joined in two stages
+]
+
+
+@pytest.mark.parametrize("case", DIVISIONS)
+def test_attention_however_the_work_is_divided(ops, seq, orc, case):
+    new, ctx, heads, kv, d, page, token_major, window, max_q = case
+    b = Batch(new, ctx, page, kv, d, "f16", 35, token_major).hide_unused()
+    op, x64, y = _attend(ops, b, "f16", heads, d, window, True, max_q)
+    ref = elastic_bitwise(op, [y], orc, bits, plans=(1, 5))
+    for _ in range(2):                         # counters are back at zero
+        y.fill_(-77.0)
+        op.run()
+        torch.cuda.synchronize()
+        assert [bits(y)] == ref
+    step = max(1, sum(new) // 60)              # rows compared: every step-th
+    want = seq.attention(x64, b.k64, b.v64, b.q_start, b.kv_len, b.table, heads, window=window, half_step=seq.HALF_STEP["f16"],
+                         p_step=_p_step(seq, "f16", max_q == 1), stride=step)
+    got = to_f64(y)
+    for r, (w, e) in want.items():
+        _inside(got[r], w, e, r)
+    assert np.all(got[sum(new):] == -77.0) and np.all(got[:sum(new)] != -77.0)
+
+
 @pytest.mark.parametrize("dtype", ["f16", "bf16"])
 @pytest.mark.parametrize("new,heads", [([4, 2], 4), ([200, 2], 4)])
 def test_rows_without_keys_give_zeros(ops, seq, dtype, new, heads):
