@@ -2,17 +2,19 @@
 //   h = residual + scale * u,   y = h,   z = N_pre(h),
 // N(v) = (v - mean) / sqrt(mean((v - mean)^2) + eps) * weight + bias, the mean 0 for RMS norm.
 //
-// What bounds it: HBM, every row read and written once.  So a row stays in registers between its passes:
-// one logical wave's for short rows, and the four of a tile's for longer ones, whose sums meet in LDS.  Rows
-// beyond 32 vectors per lane (16384 16-bit values) are read again for each pass, and so are all rows of the
-// second kind in blocks of 64 and 128, where one wave would have to hold what two or four do.
+// What bounds it: HBM, every row read and written once (8192 rows of 4096 bf16 with residual and both outputs:
+// 57 us, 4.7 TB/s, a copy 4.9).  Reading the weights once for four rows, or before the sums are known, changed nothing.  So a row
+// stays in registers between its passes: one logical wave's for short rows, and the four of a tile's for longer
+// ones, whose sums meet in LDS.  Rows beyond 32 vectors per lane (16384 16-bit values) are read again for each
+// pass, and so are all rows of the second kind in blocks of 64 and 128, where one wave would have to hold what two
+// or four do.
 //
 // Rows are whole 16-byte vectors, at any alignment with RAG, and a rest of less than one, an element of which
 // the first lanes hold besides.  Sums are fp32: each lane's own values in order, the wave's lanes in the fixed
 // order of wave_sum, then the four waves' in order; the same operations whether a row is kept or read again,
 // so results do not depend on the physical block (hence no contraction by the compiler).
 #include "memops.h"
-#include "seq_args.h"
+#include "seq_rows.h"
 
 #pragma clang fp contract(off)
 
@@ -31,14 +33,17 @@ __device__ __forceinline__ float gate_value(int kind, float g) {
 template <class T, int N, bool RAG>
 struct Held {
     Vec16<T> p;
+    template <bool PAST = false>
     __device__ __forceinline__ void load(const T *src) {
         if constexpr (N == 1) p.e[0] = *src;
-        else p = RAG ? ld_loose(src) : ld_vec(src);
+        else if constexpr (RAG) p = ld_loose(src);
+        else if constexpr (PAST) p.u = ld_past(src);
+        else p = ld_vec(src);
     }
     __device__ __forceinline__ float at(int e) const { return TypeOps<T>::to_f(p.e[e]); }
 };
 template <class T, int N, bool RAG>
-__device__ __forceinline__ void put_row(T *dst, const float (&v)[N]) {
+__device__ __forceinline__ void put_row(T *dst, const float (&v)[N], int past) {
     if constexpr (N == 1) {
         st_f(dst, v[0]);
     } else {
@@ -46,6 +51,7 @@ __device__ __forceinline__ void put_row(T *dst, const float (&v)[N]) {
 #pragma unroll
         for (int e = 0; e < N; ++e) o.e[e] = TypeOps<T>::from_f(v[e]);
         if constexpr (RAG) st_loose(dst, o);
+        else if (past) st_past(dst, o.u);
         else st_vec(dst, o);
     }
 }
@@ -103,7 +109,7 @@ __global__ __launch_bounds__(kWave * P) void norm_kernel(NormArgs a, Shard sh) {
     const int pw = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const int lane = threadIdx.x % kWave;
     const int64_t G = gridDim.x;
-    const int64_t rank = wg_rank(blockIdx.x, G);
+    const int64_t rank = a.past ? blockIdx.x : wg_rank(blockIdx.x, G);
     constexpr int64_t step = (int64_t)WR * kWave * V;
     const float inv_n = 1.0f / (float)a.n;
     const int64_t whole = RAG ? a.n / V * V : a.n;  // the rest: one element of the row's first lanes
@@ -159,11 +165,16 @@ __global__ __launch_bounds__(kWave * P) void norm_kernel(NormArgs a, Shard sh) {
                 {
                     Piece x[NR];
                     One xt;
-                    each([&](int i, int64_t j) {
-                        x[i].load(xr + j);
-                        if (a.res) r[i].load(rr + j);
-                        if (rows_gate) g[i].load(gr + j);
-                    });
+                    auto fetch = [&](auto past) {
+                        constexpr bool PAST = decltype(past)::value != 0;
+                        each([&](int i, int64_t j) {
+                            x[i].template load<PAST>(xr + j);
+                            if (a.res) r[i].template load<PAST>(rr + j);
+                            if (rows_gate) g[i].template load<PAST>(gr + j);
+                        });
+                    };
+                    if (!RAG && a.past) fetch(ActTag<1>{});
+                    else fetch(ActTag<0>{});
                     if (rest) {
                         xt.load(xr + jt);
                         if (a.res) rt.load(rr + jt);
@@ -196,21 +207,21 @@ __global__ __launch_bounds__(kWave * P) void norm_kernel(NormArgs a, Shard sh) {
                 }
                 each([&](int i, int64_t j) {
                     norm_join<V, RAG>(a, v[i], j, r[i], g[i]);
-                    if (a.y) put_row<T, V, RAG>(yr + j, v[i]);
+                    if (a.y) put_row<T, V, RAG>(yr + j, v[i], a.past);
                 });
                 if (rest) {
                     norm_join<1, RAG>(a, vt, jt, rt, gt);
-                    if (a.y) put_row<T, 1, RAG>(yr + jt, vt);
+                    if (a.y) put_row<T, 1, RAG>(yr + jt, vt, a.past);
                 }
                 if (a.z) {
                     stats(mean, rstd);
                     each([&](int i, int64_t j) {
                         norm_apply<V, RAG>(v[i], j, a.pre, a.pre_bias, mean, rstd);
-                        put_row<T, V, RAG>(zr + j, v[i]);
+                        put_row<T, V, RAG>(zr + j, v[i], a.past);
                     });
                     if (rest) {
                         norm_apply<1, RAG>(vt, jt, a.pre, a.pre_bias, mean, rstd);
-                        put_row<T, 1, RAG>(zr + jt, vt);
+                        put_row<T, 1, RAG>(zr + jt, vt, a.past);
                     }
                 }
             } else {
@@ -259,10 +270,10 @@ __global__ __launch_bounds__(kWave * P) void norm_kernel(NormArgs a, Shard sh) {
                 auto finish = [&](auto &v, int64_t j) {
                     constexpr int N = sizeof(v) / sizeof(float);
                     joined(v, j);
-                    if (a.y) put_row<T, N, RAG>(yr + j, v);
+                    if (a.y) put_row<T, N, RAG>(yr + j, v, a.past);
                     if (a.z) {
                         norm_apply<N, RAG>(v, j, a.pre, a.pre_bias, m2, r2);
-                        put_row<T, N, RAG>(zr + j, v);
+                        put_row<T, N, RAG>(zr + j, v, a.past);
                     }
                 };
                 float v[V], vt[1];

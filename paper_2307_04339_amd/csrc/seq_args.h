@@ -5,6 +5,14 @@
 
 namespace miriam {
 
+// Ops that move more than this read and write their rows past the caches: nothing would be left in L2 (8 x 4 MB) for
+// a reader anyway, and lines that are used once no longer take places from others; and their tiles go over the dies
+// in turn, so that all memory channels are busy at once.  With buffers that the last-level cache does not hold: norms
+// of 8192 rows of 4096 69 -> 57 us (outputs alone 63, tiles in turn 60), positions of 8192 tokens of 48 heads of
+// 128 49 -> 41 us (47, 45).  Norms and then a reader of both outputs, of buffers that it does hold: 134 MB 50.4 ->
+// 49.2 us, 67 MB 27.7 -> 28.9, 34 MB 21.4 -> 19.8.
+constexpr double kPastBytes = 32e6;
+
 // The norms around a block.
 struct NormArgs {
     const void *x, *res, *gate;                      // res, gate: null = none
@@ -14,6 +22,7 @@ struct NormArgs {
     float scale, eps;
     int32_t gate_kind;                               // miriam_gate
     int32_t layer;                                   // 1: layer norm, 0: RMS norm
+    int32_t past;                                    // rows are read and written past the caches (see kPastBytes)
 };
 
 // What a row is divided into: one logical wave holding 1 or 2 vectors per lane; a tile's four logical waves
@@ -41,6 +50,7 @@ struct RotaryArgs {
     int32_t heads, kv_heads, d, rot;
     int32_t interleaved;
     int32_t items, rot_items; // vector pairs per head, and those of them that are turned
+    int32_t past;             // rows are read and written past the caches (see kPastBytes)
     int32_t parts;            // logical waves per row
     FastDiv fd_parts;         // division by it
     float scale;

@@ -119,6 +119,7 @@ static int create_norm(miriam_op *op) {
     op->flops = 12.0 * e;
     op->bytes = es * e * (1.0 + (a.res ? 1 : 0) + (rows_gate ? 1 : 0) + (a.y ? 1 : 0) + (a.z ? 1 : 0)) +
                 4.0 * a.n * ((a.post ? 1 : 0) + (a.post_bias ? 1 : 0) + (a.pre ? 1 : 0) + (a.pre_bias ? 1 : 0) + (a.gate && !rows_gate ? 1 : 0));
+    a.past = op->bytes > kPastBytes;
     return MIRIAM_OK;
 }
 
@@ -171,6 +172,7 @@ static int create_rotary(miriam_op *op) {
     if (rotary_kernels(d.dtype, vec, op->kern) != 0) return einval("rotary: no kernel for this dtype");
     op->flops = 3.0 * (double)d.tokens * (double)(d.heads + d.kv_heads) * (double)d.rot;
     op->bytes = 2.0 * es * (double)d.tokens * (double)width;
+    a.past = op->bytes > kPastBytes;
     return MIRIAM_OK;
 }
 

@@ -12,6 +12,22 @@ __device__ __forceinline__ int seq_len(const SeqArgs &q, int64_t s) {
     return clampi(q.kv_len[s], 0, q.table ? q.page * q.max_pages : 0x3fffffff);
 }
 
+// Loads and stores past the caches.  (The empty statements keep the compiler from merging them with ordinary ones in
+// the other branch of a condition, which makes both ordinary.)
+template <class T>
+__device__ __forceinline__ u32x4 ld_past(const T *p) {
+    asm volatile("");
+    const u32x4 v = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(p));
+    asm volatile("");
+    return v;
+}
+template <class T>
+__device__ __forceinline__ void st_past(T *p, const u32x4 &v) {
+    asm volatile("");
+    __builtin_nontemporal_store(v, reinterpret_cast<u32x4 *>(p));
+    asm volatile("");
+}
+
 // Sequence of packed row `row` (uniform over the wave): the number of sequences that end at or before it, found
 // by all lanes at once, and its position; -1 for a row that belongs to none.
 __device__ __forceinline__ int find_seq(const SeqArgs &q, int row, int lane, int &pos) {
