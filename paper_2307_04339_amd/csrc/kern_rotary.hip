@@ -138,8 +138,12 @@ __global__ __launch_bounds__(kWave * P) void rotary_kernel(RotaryArgs a, Shard s
                         if (turns && h < turned) {
                             auto pair = [&](T &ta, T &tb, int e) {
                                 const float x = TypeOps<T>::to_f(ta), y = TypeOps<T>::to_f(tb);
-                                ta = TypeOps<T>::from_f(__builtin_fmaf(x, cs[e], -(y * sn[e])));
-                                tb = TypeOps<T>::from_f(__builtin_fmaf(y, cs[e], x * sn[e]));
+                                // (held in 32 bits: where the compiler made one instruction of the sum and its rounding
+                                // to fp16, in some of the unrolled copies only, some results differed by a step)
+                                float ra = __builtin_fmaf(x, cs[e], -(y * sn[e])), rb = __builtin_fmaf(y, cs[e], x * sn[e]);
+                                asm("" : "+v"(ra), "+v"(rb));
+                                ta = TypeOps<T>::from_f(ra);
+                                tb = TypeOps<T>::from_f(rb);
                             };
                             if (V == 1 || !a.interleaved) {
 #pragma unroll

@@ -111,6 +111,25 @@ def test_block_norm_of_large_and_zero_rows(ops, seq):
     assert np.all(z[0] == 0) and np.allclose(z[1], 1.0, rtol=1e-5) and np.allclose(z[2], 3e-30 / np.sqrt(1e-5), rtol=1e-5)
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("m,n", [(6000, 768), (1100, 4096), (260, 16640), (5003, 1001)])
+def test_block_norm_of_more_than_the_caches_hold(ops, orc, dtype, m, n):
+    """Large ops move their rows past the caches: the bits of small ones over the same rows."""
+    x, r, g = (rand((m, n), dtype, 30 + i)[0] for i in range(3))
+    w = [f32_dev(np.random.default_rng(33 + i).uniform(-1, 1, n)) for i in range(2)]
+    y, z = sentinel((m, n), dtype), sentinel((m, n), dtype)
+    make = lambda a, b: ops.block_norm(x[a:b], y[a:b], residual=r[a:b], post=w[0], gate=g[a:b], gate_act="silu", z=z[a:b], pre=w[1])  # noqa: E731
+    op = make(0, m)
+    assert 5 * m * n * x.element_size() > 32e6
+    ref = elastic_bitwise(op, [y, z], orc, bits, plans=(1, 3), blocks=(64, 256))
+    y.fill_(-77.0)
+    z.fill_(-77.0)
+    for a in range(0, m, 251):
+        make(a, min(m, a + 251)).run()
+    torch.cuda.synchronize()
+    assert [bits(y), bits(z)] == ref
+
+
 # ---------------------------------------------------------------------- rotary
 ROTARY_CASES = [
     # new, ctx, heads, kv_heads, d, rot, page, token_major, interleaved, scale
@@ -166,6 +185,35 @@ def test_rotary_and_append(ops, seq, orc, dtype, case):
         assert np.all(g.transpose(0, 2, 1, 3)[~written] == -77.0)
     assert len(kv_at) == sum(new)
     elastic_bitwise(op, [y, b.k, b.v], orc, bits)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("inter,d", [(False, 128), (True, 128), (False, 90)])
+def test_rotary_of_more_than_the_caches_hold(ops, orc, dtype, inter, d):
+    """Large ops move their rows past the caches: the bits of small ones over the same tokens."""
+    heads, kv, new = 24, 4, [2000, 1, 999]
+    b = Batch(new, [2500, 1, 1000], 16, kv, d, dtype, 25, behind=0)
+    x, _ = rand((b.tokens, (heads + 2 * kv) * d), dtype, 26)
+    y = sentinel((b.tokens, heads * d), dtype)
+    q_start, kv_len, table = b.arrays()
+    freq = ops.rotary_freqs(d // 2 * 2).cuda()
+    op = ops.rotary(x, y, freq, q_start, kv_len, heads=heads, head_dim=d, kv_heads=kv, k_cache=b.k, v_cache=b.v, page_table=table,
+                    interleaved=inter)
+    assert 2 * x.numel() * x.element_size() > 32e6
+    ref = elastic_bitwise(op, [y, b.k, b.v], orc, bits, plans=(1, 3), blocks=(64, 256))
+    for t in (y, b.k, b.v):
+        t.fill_(-77.0)
+    at = 0
+    for s, n in enumerate(new):                # pieces of a sequence's tokens, each at the end of its cache
+        for i in range(0, n, 500):
+            m = min(500, n - i)
+            part = torch.tensor([0, m], dtype=torch.int32, device="cuda")
+            length = torch.tensor([b.ctx[s] - n + i + m], dtype=torch.int32, device="cuda")
+            ops.rotary(x[at:at + m], y[at:at + m], freq, part, length, heads=heads, head_dim=d, kv_heads=kv, k_cache=b.k,
+                       v_cache=b.v, page_table=table[s:s + 1], interleaved=inter).run()
+            at += m
+    torch.cuda.synchronize()
+    assert [bits(t) for t in (y, b.k, b.v)] == ref
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
