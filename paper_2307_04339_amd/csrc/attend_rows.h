@@ -63,46 +63,58 @@ __global__ __launch_bounds__(kWave * P, DP > 128 ? 1 : 2) void attend_rows_kerne
     // rows but no keys, to write their zeros), their places in the list, and the places up to and with them.
     SeqView view;
     int base = 0, blocks = 0, mine = 0, upto = 0;
+    auto blocks_of = [&](const SeqView &v) {
+        const int n = (v.end + kRowKeys - 1) / kRowKeys - v.begin / kRowKeys;
+        return v.n <= 0 ? 0 : n > 0 ? n : 1;
+    };
     auto look = [&](int from) {
         base = from;
-        blocks = 0;
         view = SeqView{};
         if (base + lane < seqs) view = seq_view(a, base + lane);
-        if (view.n > 0) {
-            const int n = (view.end + kRowKeys - 1) / kRowKeys - view.begin / kRowKeys;
-            blocks = n > 0 ? n : 1;
+        blocks = blocks_of(view);
+    };
+    auto upto_lane = [&](int n) {  // the sum over the lanes up to and with this one
+#pragma unroll
+        for (int o = 1; o < kWave; o <<= 1) {
+            const int v = __shfl_up(n, o);
+            n += lane >= o ? v : 0;
         }
+        return n;
     };
     // All blocks, and each tile's share.  While there are tiles enough for runs of two blocks that do not cross
     // from one head into the next, these are taken (a head's list then counts as even): two blocks take little
     // longer than one, and most heads of short sequences need no joining.
-    int total = 0, share = 0;
+    int total = 0, share = 0, ahead = 0;  // ahead: places up to and with the lane's part of the sequences
     bool even = false;
+    const int per = (seqs + kWave - 1) / kWave;  // sequences of a lane's part (300 of 300 keys, one cache head: 49 us, 64 after 64: 61)
     if (a.splits > 1) {
         int sum = 0, pairs = 0;
-        for (int from = (seqs - 1) / kWave * kWave; from >= 0; from -= kWave) {  // (the first 64 stay)
-            look(from);
-            sum += blocks;
-            pairs += (blocks + 1) / 2;
+        if (per == 1) {
+            look(0);  // (they stay)
+            sum = blocks;
+            pairs = (blocks + 1) / 2;
+        } else {
+            for (int s = lane * per; s < (lane + 1) * per && s < seqs; ++s) {
+                const int n = blocks_of(seq_view(a, s));
+                sum += n;
+                pairs += (n + 1) / 2;
+            }
         }
+        int all = sum, all_pairs = pairs;
         for (int o = 32; o > 0; o >>= 1) {
-            sum += __shfl_xor(sum, o);
-            pairs += __shfl_xor(pairs, o);
+            all += __shfl_xor(all, o);
+            all_pairs += __shfl_xor(all_pairs, o);
         }
-        total = __builtin_amdgcn_readfirstlane(sum) * heads;
-        pairs = __builtin_amdgcn_readfirstlane(pairs) * heads;
-        even = pairs <= (int)a.T;
-        if (even) total = 2 * pairs;
+        total = __builtin_amdgcn_readfirstlane(all) * heads;
+        all_pairs = __builtin_amdgcn_readfirstlane(all_pairs) * heads;
+        even = all_pairs <= (int)a.T;
+        if (even) total = 2 * all_pairs;
         share = even ? 2 : (total + (int)a.T - 1) / (int)a.T;
+        ahead = upto_lane((even ? 2 * pairs : sum) * heads);
     }
     auto list = [&]() {
         mine = (even ? (blocks + 1) & ~1 : blocks) * heads;
-        upto = mine;
-#pragma unroll
-        for (int o = 1; o < kWave; o <<= 1) {
-            const int v = __shfl_up(upto, o);
-            upto += lane >= o ? v : 0;
-        }
+        upto = upto_lane(mine);
     };
     auto view_of = [&](int i) {  // of the 64's i-th
         SeqView v;
@@ -421,8 +433,14 @@ __global__ __launch_bounds__(kWave * P, DP > 128 ? 1 : 2) void attend_rows_kerne
         const int stop = at + share < total ? at + share : total;
         if (at >= stop) continue;
         // the sequence of place `at`
-        if (base != 0) look(0);
         int before = 0;  // places before the 64
+        if (per > 1) {
+            const int p = __builtin_popcountll(__ballot(ahead <= at));
+            before = p > 0 ? __builtin_amdgcn_readlane(ahead, p - 1) : 0;
+            look(p * per);
+        } else if (base != 0) {
+            look(0);
+        }
         for (list(); base < seqs; list()) {
             const int all = __builtin_amdgcn_readlane(upto, kWave - 1);
             if (before + all > at) break;

@@ -17,7 +17,7 @@
 //    a tile each, as the hardware hands them out.
 //  - Fewer row tiles than such workgroups, of like lengths (a chunk behind a long context): every row tile is cut
 //    into about equal pieces, at the same keys for all row tiles of a sequence, which then share them in L2
-//    (512 tokens behind 16k: 178 us, in equal runs of the list below 205).
+//    (512 tokens behind 16k: 174 us, in equal runs of the list below 205).
 //  - Otherwise (single tokens beside chunks): the steps of all row tiles form a list of which every tile takes an
 //    equal run (20 sequences of 1 to 400 tokens: 61 us, in pieces 70, a fixed division of every row tile 86).  As
 //    a second row tile's start and the joining cost more than a few steps, a run's end that lies within a third of
@@ -59,7 +59,7 @@ __global__ __launch_bounds__(kWave * P, DP > 128 ? 1 : 2) void attend_tile_kerne
     typedef typename MF::acc_t acc_t;
     constexpr int NJ = K_::NJ, ND = K_::ND, CPR = K_::CPR, RPL = K_::RPL, NLD = K_::NLD;
     __shared__ __attribute__((aligned(1024))) char smem[K_::LDS_BYTES];
-    __shared__ int s_last;
+    __shared__ int s_last, s_ahead[kWave];
     lds_char const lsmem = (lds_char)smem;
     // where the lane reads the values of output tile i in a stage, and the keys of step j: the swizzles go by the
     // lane alone
@@ -126,6 +126,47 @@ __global__ __launch_bounds__(kWave * P, DP > 128 ? 1 : 2) void attend_tile_kerne
         }
         return n;
     };
+    // row tiles of a cache head, the longest sequence's steps, and at least half of all; a lane goes through its part
+    // of the sequences, so that a tile need not look through all of them again (1000 sequences of 128 tokens, 12
+    // heads of 64: 446 us, 64 sequences after 64 twice 581)
+    const int per = (seqs + kWave - 1) / kWave;
+    int J = 0, longest = 0;
+    float half = 0.0f;
+    {
+        auto add = [&](const SeqView &v) {
+            const int nt = (v.n * g + kTileRows - 1) / kTileRows;
+            const int n = nt > 0 && v.end > v.begin ? (v.end + kTileKeys - 1) / kTileKeys - v.begin / kTileKeys : 0;
+            J += nt;
+            longest = longest > n ? longest : n;
+            half += 0.5f * (float)n * (float)nt;
+        };
+        if (per == 1) {
+            look(0);  // (they stay)
+            add(view);
+        } else {
+            for (int s = lane * per; s < (lane + 1) * per && s < seqs; ++s) add(seq_view(a, s));
+        }
+        const int ahead = scan(J);  // row tiles up to and with the lane's part
+        if (pw == 0) s_ahead[lane] = ahead;
+        J = __builtin_amdgcn_readlane(ahead, kWave - 1);
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) {
+            const int v = __shfl_xor(longest, o);
+            longest = longest > v ? longest : v;
+            half += __shfl_xor(half, o);
+        }
+        longest = __builtin_amdgcn_readfirstlane(longest);
+        __syncthreads();
+    }
+    // where to look for row tile j: the first sequence of its part, and the row tiles before that
+    auto part_of = [&](int j, int &from, int &before) {
+        from = before = 0;
+        if (per > 1) {
+            const int ahead = s_ahead[lane], p = __builtin_popcountll(__ballot(ahead <= j));
+            from = p * per;
+            before = p > 0 ? __builtin_amdgcn_readlane(ahead, p - 1) : 0;
+        }
+    };
     // row tiles 64 c .. 64 c + 63 of a cache head, one per lane: whose, which of its, and its steps (0: none)
     struct Chunk {
         int s, qi, n;
@@ -134,7 +175,8 @@ __global__ __launch_bounds__(kWave * P, DP > 128 ? 1 : 2) void attend_tile_kerne
     auto chunk = [&](int c) {
         Chunk r = {};
         const int want = c * kWave + lane;
-        for (int from = 0, before = 0; from < seqs; from += kWave) {
+        int from, before;
+        for (part_of(c * kWave, from, before); from < seqs; from += kWave) {
             look(from);
             const int upto = scan(ntiles), all = __builtin_amdgcn_readlane(upto, kWave - 1);
             int i = 0;  // sequences of these that end at or before it
@@ -157,26 +199,6 @@ __global__ __launch_bounds__(kWave * P, DP > 128 ? 1 : 2) void attend_tile_kerne
         }
         return r;
     };
-    // row tiles of a cache head, the longest sequence's steps, and at least half of all
-    int J = 0, longest = 0;
-    float half = 0.0f;
-    for (int from = (seqs - 1) / kWave * kWave; from >= 0; from -= kWave) {  // (the first 64 stay)
-        look(from);
-        int k = ntiles, n = ntiles > 0 && view.end > view.begin ? (view.end + kTileKeys - 1) / kTileKeys - view.begin / kTileKeys : 0;
-        float h = 0.5f * (float)n * (float)ntiles;
-#pragma unroll
-        for (int o = 32; o > 0; o >>= 1) {
-            const int v = __shfl_xor(n, o);
-            n = v > n ? v : n;
-            k += __shfl_xor(k, o);
-            h += __shfl_xor(h, o);
-        }
-        J += k;
-        longest = longest > n ? longest : n;
-        half += h;
-    }
-    J = __builtin_amdgcn_readfirstlane(J);
-    longest = __builtin_amdgcn_readfirstlane(longest);
     const bool many = J * a.kv_heads >= 4 * a.runs && (float)longest * (float)a.runs <= 2.0f * half * (float)a.kv_heads;
     // (more row tiles than rows can have: starts that overlap; no tile may then wait for another's part)
     const bool list = a.splits > 1 && J <= a.tiles && !__builtin_amdgcn_readfirstlane(many);
@@ -267,7 +289,8 @@ __global__ __launch_bounds__(kWave * P, DP > 128 ? 1 : 2) void attend_tile_kerne
                 }
             }
         } else {
-            for (int from = 0, before = 0; from < seqs && s < 0; from += kWave) {
+            int from, before;
+            for (part_of(j, from, before); from < seqs && s < 0; from += kWave) {
                 look(from);
                 const int upto = scan(ntiles), all = __builtin_amdgcn_readlane(upto, kWave - 1);
                 if (j - before < all) {
