@@ -223,6 +223,7 @@ def _rows(name, t, width=None, rows=None, dtype=None):
     _need(rows is None or t.shape[0] == rows, f"{name}: {rows} rows expected, got {t.shape[0]}")
     _need(dtype is None or t.dtype == dtype, f"{name}: {dtype} expected, got {t.dtype}")
     # (the stride of a single row says nothing)
+    _need(t.shape[0] <= 1 or t.stride(0) >= t.shape[1], f"{name}: rows that share memory (a broadcast tensor?)")
     return t.stride(0) if t.shape[0] > 1 else t.shape[1]
 
 
@@ -256,6 +257,7 @@ def _sequences(q_start, kv_len, page_table, k_cache, v_cache, dtype):
     _need(k_cache.shape[3] == 1 or k_cache.stride(3) == 1, "caches: the values of a head must be adjacent")
     _need(page_table.dim() == 2 and page_table.shape[0] == seqs and page_table.dtype == torch.int32 and
           (page_table.shape[1] <= 1 or page_table.stride(1) == 1), f"page_table: {seqs} rows of adjacent int32 expected")
+    _need(seqs <= 1 or page_table.stride(0) >= page_table.shape[1], "page_table: rows that share memory (a broadcast tensor?)")
     f.update(kv_heads=k_cache.shape[1], page=k_cache.shape[2], pages=k_cache.shape[0], max_pages=page_table.shape[1],
              ldt=page_table.stride(0) if seqs > 1 else page_table.shape[1], page_table=page_table, k_cache=k_cache,
              v_cache=v_cache, cache_page=k_cache.stride(0), cache_head=k_cache.stride(1), cache_token=k_cache.stride(2))

@@ -191,6 +191,20 @@ def test_tensors_that_do_not_fit_are_refused():
 
 
 # ------------------------------------------------------------------- the oracle
+def test_broadcast_rows_are_refused():
+    """A row stride of 0 means dense rows to the library, and rows closer than their width are none."""
+    from paper_2307_04339_amd import ops
+    x = torch.zeros(64)
+    for t in (x.expand(5, 64), x.as_strided((3, 16), (8, 1))):
+        with pytest.raises(ValueError, match="share memory"):
+            ops._rows("x", t)
+    assert ops._rows("x", x.expand(1, 64)) == 64 and ops._rows("x", x.view(4, 16)[:, :8]) == 16
+    c, i = torch.zeros(2, 1, 16, 64), lambda n: torch.zeros(n, dtype=torch.int32)  # noqa: E731
+    with pytest.raises(ValueError, match="share memory"):
+        ops._sequences(i(4), i(3), i(2).expand(3, 2), c, c.clone(), torch.float32)
+    assert ops._sequences(i(2), i(1), i(2).expand(1, 2), c, c.clone(), torch.float32)["ldt"] == 2
+
+
 def test_oracle_attention_against_a_masked_softmax():
     rng = np.random.default_rng(1)
     page, kv, d, heads = 4, 2, 8, 6
