@@ -49,6 +49,9 @@ static int check_seqs(const miriam_seq_desc &d, SeqArgs &q, bool cache) {
     if (q.ldt < d.max_pages) return einval("page table: row stride too small");
     if (d.cache_page < 1 || d.cache_head < 1 || d.cache_token < 1) return einval("cache strides must be >= 1");
     if (d.page > 1 && d.cache_token < d.head_dim) return einval("cache: token stride smaller than a head");
+    constexpr int64_t far = (int64_t)1 << 58;  // bytes of a cache stay below 2^62
+    if (d.cache_page > far / d.pages || d.cache_head > far / std::max<int64_t>(d.kv_heads, 1) || d.cache_token > far / d.page)
+        return einval("cache strides are too large");
     q.table = d.page_table;
     q.sp = d.cache_page;
     q.sh = d.cache_head;
@@ -58,6 +61,12 @@ static int check_seqs(const miriam_seq_desc &d, SeqArgs &q, bool cache) {
     q.max_pages = (int32_t)d.max_pages;
     q.fd_page = make_fastdiv((uint32_t)d.page);
     return MIRIAM_OK;
+}
+
+// A cache from its first value to its last (with the other one in between where they are interleaved).
+static Rows cache_span(const miriam_seq_desc &d, const void *p, int es) {
+    const int64_t n = (d.pages - 1) * d.cache_page + (d.kv_heads - 1) * d.cache_head + (d.page - 1) * d.cache_token + d.head_dim;
+    return {p, 1, n, n, es};
 }
 
 // The heads of a descriptor.
@@ -104,6 +113,8 @@ static int create_norm(miriam_op *op) {
     const Rows y{a.y, a.rows, a.n, a.ldy, es}, z{a.z, a.rows, a.n, a.ldz, es};
     for (const Rows &in : ins)
         if (overlap(in, y) || overlap(in, z)) return einval("block norm: an output overlaps an input");
+    for (const float *w : {d.post, d.post_bias, d.pre, d.pre_bias, rows_gate ? nullptr : static_cast<const float *>(d.gate)})
+        if (overlap({w, 1, a.n, a.n, 4}, y) || overlap({w, 1, a.n, a.n, 4}, z)) return einval("block norm: an output overlaps weights");
     if (overlap(y, z)) return einval("block norm: y and z overlap");
     // 16-byte vectors, or pieces at any alignment with the last one by element
     const bool vec = d.n % V == 0 && a.ldx % V == 0 && aligned(a.x, 16) && (!a.res || (a.ldr % V == 0 && aligned(a.res, 16))) &&
@@ -151,6 +162,11 @@ static int create_rotary(miriam_op *op) {
         if (!aligned(p, (uintptr_t)es)) return einval("rotary: x, y and the caches must be aligned to their type");
     const Rows x{a.x, d.tokens, width, a.ldx, es}, y{a.y, d.tokens, d.heads * d.head_dim, a.ldy, es};
     if (overlap(x, y)) return einval("rotary: y overlaps x");
+    if (d.kv_heads > 0) {
+        const Rows k = cache_span(d, a.k, es), v = cache_span(d, a.v, es);
+        if (a.k == a.v) return einval("rotary: both caches are one");
+        if (overlap(x, k) || overlap(x, v) || overlap(y, k) || overlap(y, v)) return einval("rotary: x or y overlaps a cache");
+    }
     a.heads = (int32_t)d.heads; a.kv_heads = (int32_t)d.kv_heads; a.d = (int32_t)d.head_dim; a.rot = (int32_t)d.rot;
     a.interleaved = (d.flags & MIRIAM_SEQ_INTERLEAVED) ? 1 : 0;
     a.scale = d.scale;
@@ -201,7 +217,9 @@ static int create_attention(miriam_op *op) {
     if (!aligned(a.x, 16) || !aligned(a.y, 16) || !aligned(a.k, 16) || !aligned(a.v, 16) || a.ldx % 8 != 0 || a.ldy % 8 != 0 ||
         a.sq.sp % 8 != 0 || a.sq.sh % 8 != 0 || a.sq.st % 8 != 0)
         return einval("attention: x, y and the caches must be 16-byte aligned, their strides multiples of 8");
-    if (overlap({a.x, d.tokens, width, a.ldx, 2}, {a.y, d.tokens, width, a.ldy, 2})) return einval("attention: y overlaps x");
+    const Rows y{a.y, d.tokens, width, a.ldy, 2};
+    if (overlap({a.x, d.tokens, width, a.ldx, 2}, y)) return einval("attention: y overlaps x");
+    if (overlap(y, cache_span(d, a.k, 2)) || overlap(y, cache_span(d, a.v, 2))) return einval("attention: y overlaps a cache");
     a.heads = (int32_t)d.heads; a.kv_heads = (int32_t)d.kv_heads; a.group = (int32_t)(d.heads / d.kv_heads); a.d = (int32_t)d.head_dim;
     a.fd_group = make_fastdiv((uint32_t)a.group);
     a.fd_kv = make_fastdiv((uint32_t)a.kv_heads);
@@ -209,6 +227,7 @@ static int create_attention(miriam_op *op) {
     a.window = (int32_t)std::min<int64_t>(d.window, kMost);
     a.causal = (d.flags & MIRIAM_SEQ_CAUSAL) ? 1 : 0;
     a.scale = (float)((double)d.scale * 1.4426950408889634074);
+    if (!std::isfinite(a.scale)) return einval("attention: scale is too large");
     const bool rows = (int64_t)a.max_q * a.group <= 16;
     const int dp = d.head_dim <= 64 ? 64 : d.head_dim <= 128 ? 128 : 256;
     const int64_t cus = device_cus(), part = attend_partial(rows ? 16 : kTileRows, dp) * 4, keys = d.page * d.max_pages;

@@ -98,6 +98,28 @@ def test_refusals(L, base, changes):
     assert L.load().miriam_last_error()
 
 
+@pytest.mark.parametrize("base,changes", [(b, c) for b, cs in [
+    (NORM, [dict(y=_at(6)), dict(z=_at(5) - 64), dict(post_bias=_at(9), y=_at(9) + 16), dict(gate=_at(9), gate_kind=1, z=_at(9) + 764 * 4),
+            dict(pre_bias=_at(9), z=_at(9) - 10 * 768 * 2 + 2)]),
+    (ROT, [dict(v_cache=_at(3)), dict(x=_at(3)), dict(y=_at(4)), dict(y=_at(3) - 64), dict(x=_at(4) + 2 * 2048 * 7), dict(cache_page=1 << 60),
+           dict(cache_head=1 << 62), dict(cache_token=1 << 60)]),
+    (ATT, [dict(y=_at(3)), dict(y=_at(4) - 512), dict(y=_at(4) + 2 * (2048 * 7 + 1024 + 15 * 64)), dict(scale=3e38), dict(cache_page=1 << 60)]),
+] for c in cs])
+def test_overlaps_and_sizes_are_refused(L, base, changes):
+    test_refusals(L, base, changes)
+
+
+@pytest.mark.parametrize("base,changes", [
+    (NORM, dict(post=_at(2) + 10 * 768 * 2)),                 # right behind the output
+    (ROT, dict(v_cache=_at(3) + 2048, cache_page=4096)),      # keys and values of a page one after the other
+    (ATT, dict(x=_at(3), v_cache=_at(3), y=_at(3) + 2 * 2048 * 8)),   # only read: may share memory
+])
+def test_neighbours_are_no_overlap(L, base, changes):
+    rc, h = _create(L, **dict(base, **changes))
+    assert rc == 0, L.load().miriam_last_error()
+    L.load().miriam_op_destroy(h)
+
+
 def test_null_arguments(L):
     h = ctypes.c_void_p()
     for fn in (L.load().miriam_seq_op_create, L.load().miriam_seq_op_create_noalloc):
