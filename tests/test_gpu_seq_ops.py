@@ -557,6 +557,55 @@ def test_another_stream(ops):
     assert bits(y) == ref
 
 
+def test_one_graph_over_every_division(ops):
+    """A chunk in pieces, runs of a list, a tile per row tile, single tokens: one captured op, batch after batch."""
+    heads, d, seqs, ctx = 32, 64, 70, 20000
+    x, _ = rand((2200, heads * d), "bf16", 200, -2, 2)
+    pages = 700
+    k, v = (rand((pages, heads, 32, d), "bf16", 201 + i)[0] for i in range(2))
+    table = torch.from_numpy(np.random.default_rng(203).integers(0, pages, (seqs, ctx // 32)).astype(np.int32)).cuda()
+    y = sentinel((2200, heads * d), "bf16")
+    zero = [0] * seqs
+    sets = [([1000] + zero[1:], [6000] + zero[1:]), ([1] * 60 + [300, 300] + zero[62:], [40] * 61 + [ctx] + zero[62:]),
+            ([30] * 70, [40 + i for i in range(70)]), ([1] * 70, [1 + i for i in range(70)]), (zero, [7] * 70)]
+    batches = [(torch.tensor(np.concatenate([[0], np.cumsum(n)]), dtype=torch.int32), torch.tensor(c, dtype=torch.int32)) for n, c in sets]
+    q_start, kv_len = (t.cuda() for t in batches[0])
+    op = ops.attention(x, k, v, y, q_start, kv_len, table, heads=heads)
+    assert op.info.ksplit > 1
+    eager = []
+    for vals in batches:
+        q_start.copy_(vals[0])
+        kv_len.copy_(vals[1])
+        y.fill_(-77.0)
+        ops.attention(x, k, v, y, q_start, kv_len, table, heads=heads).run()   # (its workspace is its own)
+        torch.cuda.synchronize()
+        eager.append(bits(y))
+    assert len(set(eager)) == len(sets)
+    _replayed(op, y, (q_start, kv_len), batches, eager)
+
+
+@pytest.mark.parametrize("max_q", [1, None])
+def test_two_operators_at_once(ops, max_q):
+    """Operators of their own workspaces on two streams, over the same caches."""
+    new, ctx = ([1] * 6, [9000, 40, 5000, 7000, 1, 333]) if max_q else ([200, 1, 70], [8000, 3000, 70])
+    b = Batch(new, ctx, 32, 2, 128, "f16", 210)
+    made = [_attend(ops, b, "f16", 8, 128, 0, True, max_q, seed=211 + i) for i in range(2)]
+    ref = []
+    for op, _, y in made:
+        op.run()
+        torch.cuda.synchronize()
+        ref.append(bits(y))
+        y.fill_(-77.0)
+    assert ref[0] != ref[1] and made[0][0].info.ksplit > 1
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    for _ in range(10):
+        for (op, _, _), s in zip(made, streams):
+            op.run(s)
+    torch.cuda.synchronize()
+    assert [bits(y) for _, _, y in made] == ref
+
+
 # -------------------------------------------------- the operators one after another
 class Layer:
     """A decoder layer's step over a paged cache: norms, projections, rotary and append, attention, gated block."""
