@@ -17,14 +17,14 @@
 //    a tile each, as the hardware hands them out.
 //  - Fewer row tiles than such workgroups, of like lengths (a chunk behind a long context): every row tile is cut
 //    into about equal pieces, at the same keys for all row tiles of a sequence, which then share them in L2
-//    (512 tokens behind 16k: 174 us, in equal runs of the list below 205).
+//    (512 tokens behind 16k: 163 us; in equal runs of the list below 205, when these took 178).
 //  - Otherwise (single tokens beside chunks): the steps of all row tiles form a list of which every tile takes an
-//    equal run (20 sequences of 1 to 400 tokens: 61 us, in pieces 70, a fixed division of every row tile 86).  As
+//    equal run (20 sequences of 1 to 400 tokens: 59 us; in pieces 70 and by a fixed division of every row tile 86, when these took 61).  As
 //    a second row tile's start and the joining cost more than a few steps, a run's end that lies within a third of
 //    a run of a row tile's is moved there.
 // A row tile that ends up in several tiles is joined by the last of them to arrive, in their order.
 //
-// 4 prompts of 4096 tokens, 32 heads of 128: 690 to 715 us, 770 to 800 TFLOP/s of the products that are needed.  The
+// 4 prompts of 4096 tokens, 32 heads of 128: 640 us, 860 TFLOP/s of the products that are needed.  The
 // matrix instructions and their operands' reads from LDS alone take 485 us, the powers of two another 110.
 #pragma once
 
@@ -363,8 +363,11 @@ __global__ __launch_bounds__(kWave * P, DP > 128 ? 1 : 2) void attend_tile_kerne
         auto slot_at = [&](int w) { return (uint32_t)(2 * w + (w == w0 ? 1 : 0)) * (uint32_t)(attend_partial(kTileRows, DP) * 4); };  // run w's partial result
         const T *const kh = static_cast<const T *>(a.k) + (int64_t)hk * a.sq.sh, *const vh = static_cast<const T *>(a.v) + (int64_t)hk * a.sq.sh;
 
-        // Page-table entries of a step: UNI: of its load (lane mod NLD), else of the lane's rows and of key `lane`.
+        // Page-table entries of a step: UNI: of load `mine`, so that a wave's i-th load is that of its lane i P; else
+        // of the lane's rows and of key `lane`.
         constexpr int NE = UNI ? 1 : K_::NI + 1;
+        const int mine = ((lane & ~(P - 1)) | ((lane + pw) & (P - 1))) % NLD;
+        const int32_t *const pages = a.sq.table + s * a.sq.ldt;
         struct Entry {
             int32_t id[NE], slot[NE];
         };
@@ -373,40 +376,47 @@ __global__ __launch_bounds__(kWave * P, DP > 128 ? 1 : 2) void attend_tile_kerne
                 n.id[i] = -1;
                 n.slot[i] = 0;
                 if (b < b1 && j < tv.end && (UNI ? j + RPL > tv.begin : j >= tv.begin)) {
-                    const int pg = (int)fdiv((uint32_t)j, a.sq.fd_page);
-                    n.slot[i] = j - pg * a.sq.page;
-                    if (pg < a.sq.max_pages) n.id[i] = a.sq.table[s * a.sq.ldt + pg];
+                    const uint32_t pg = fdiv((uint32_t)j, a.sq.fd_page);
+                    n.slot[i] = j - (int)pg * a.sq.page;
+                    if (pg < (uint32_t)a.sq.max_pages) n.id[i] = pages[pg];
                 }
             };
             if constexpr (UNI) {
-                entry(b * kTileKeys + lane % NLD * RPL, 0);
+                entry(b * kTileKeys + mine * RPL, 0);
             } else {
 #pragma unroll
                 for (int i = 0; i < K_::NI; ++i) entry(b * kTileKeys + (i * P + pw) * RPL + lane / CPR, i);
                 entry(b * kTileKeys + lane, K_::NI);
             }
         };
-        // Where a step's keys and values lie (byte offsets, -1: nowhere), and which of its keys are there.
+        // Where a step's keys and values lie (byte offsets, -1: nowhere; UNI: and how many bytes from there on), and
+        // which of its keys are there.
         struct Where {
             int64_t off[UNI ? 1 : K_::NI];
+            uint32_t bytes;
             uint64_t there;
         };
         auto resolve = [&](int b, const Entry &n) {
             Where w;
-#pragma unroll
-            for (int i = 0; i < (UNI ? 1 : K_::NI); ++i) {
-                const bool ok = n.id[i] >= 0 && n.id[i] < a.sq.pages;
-                w.off[i] = ok ? (n.id[i] * a.sq.sp + (int64_t)n.slot[i] * a.sq.st) * 2 : -1;
-            }
+            w.bytes = 0;
             if constexpr (UNI) {
-                const uint64_t groups = __ballot(w.off[0] >= 0);
+                const bool ok = (uint32_t)n.id[0] < (uint32_t)a.sq.pages;
+                w.off[0] = ((uint64_t)(uint32_t)n.id[0] * (uint64_t)a.sq.sp + (uint64_t)(uint32_t)n.slot[0] * (uint64_t)a.sq.st) * 2;
+                // rows up to the last key
+                w.bytes = ok ? (uint32_t)clampi(tv.end - (b * kTileKeys + mine * RPL), 0, RPL) * ((uint32_t)a.sq.st * 2u) : 0u;
+                const uint64_t groups = __ballot(ok);
                 constexpr uint64_t ALL = (1ull << NLD) - 1;
                 w.there = ~0ull;
                 if ((groups & ALL) != ALL || b * kTileKeys < tv.begin || (b + 1) * kTileKeys > tv.end) {
-                    const int j = b * kTileKeys + lane;
-                    w.there = __ballot(((groups >> (lane / RPL)) & 1) && j >= tv.begin && j < tv.end);
+                    const int j = b * kTileKeys + lane, q = lane / RPL, at = (q & ~(P - 1)) | ((q - pw) & (P - 1));
+                    w.there = __ballot(((groups >> at) & 1) && j >= tv.begin && j < tv.end);
                 }
             } else {
+#pragma unroll
+                for (int i = 0; i < K_::NI; ++i) {
+                    const bool ok = n.id[i] >= 0 && n.id[i] < a.sq.pages;
+                    w.off[i] = ok ? (n.id[i] * a.sq.sp + (int64_t)n.slot[i] * a.sq.st) * 2 : -1;
+                }
                 w.there = __ballot(n.id[K_::NI] >= 0 && n.id[K_::NI] < a.sq.pages);
             }
             return w;
@@ -429,11 +439,9 @@ __global__ __launch_bounds__(kWave * P, DP > 128 ? 1 : 2) void attend_tile_kerne
             for (int i = 0; i < K_::NI; ++i) {
                 const int q = i * P + pw;
                 if constexpr (UNI) {
-                    const int32_t hi = __builtin_amdgcn_readlane((int)(w.off[0] >> 32), q);
-                    const uint64_t o = ((uint64_t)(uint32_t)hi << 32) | (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)w.off[0], q);
-                    const int n = clampi(tv.end - (b * kTileKeys + q * RPL), 0, RPL);  // rows up to the last key
-                    const uint32_t bytes = hi >= 0 ? (uint32_t)n * (uint32_t)a.sq.st * 2u : 0u;
-                    buf_dma16(at[i % K_::NSW], make_rsrc(reinterpret_cast<const char *>(base) + (hi >= 0 ? o : 0), bytes), 0u, dst + (uint32_t)(q * 1024));
+                    const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)w.off[0], i * P), hi = (uint32_t)__builtin_amdgcn_readlane((int)(w.off[0] >> 32), i * P);
+                    const uint32_t bytes = (uint32_t)__builtin_amdgcn_readlane((int)w.bytes, i * P);
+                    buf_dma16(at[i % K_::NSW], make_rsrc(reinterpret_cast<const char *>(base) + (((uint64_t)hi << 32) | lo), bytes), 0u, dst + (uint32_t)(q * 1024));
                 } else {
                     const uint32_t d = at[i % K_::NSW];
                     const bool ok = w.off[i] >= 0 && d != kOutOfRange;
