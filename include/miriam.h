@@ -277,10 +277,12 @@ int miriam_op_destroy(miriam_op *op);
  * of any lengths within its capacities.  They are clamped there, so that no value of theirs leads outside the
  * buffers: starts to 0 .. tokens, lengths to 0 .. max_pages * page; a page outside 0 .. pages - 1 is absent:
  * its keys are not there for any query and nothing is stored to it.  Rows that belong to no sequence are left
- * as they were.
+ * as they were.  The arrays must hold one batch from the first launch of a pass to its last: how the tiles divide
+ * the work follows from them.
  *
  * The coordinator runs an operator several times when it measures it, so none of these works in place: an
- * output that overlaps an input is refused (columns of their own in rows of one buffer are no overlap).
+ * output that overlaps rows, weights or caches that are read is refused (columns of their own in rows of one
+ * buffer are no overlap); ROTARY wants two caches, which may be interleaved.
  */
 typedef enum {
     /* Norms around a block, with its gate and residual, over rows of n values:
@@ -302,11 +304,14 @@ typedef enum {
      * query head, heads / kv_heads consecutive ones sharing a cache head, over the keys j < kv_len[s] that
      * are there and, with MIRIAM_SEQ_CAUSAL, at or before the token's position, and with window > 0 among the
      * `window` last ones up to it.  A row without keys gives zeros, and what a row does not see never reaches
-     * it, whatever it holds (infinities and NaN included).  fp16 / bf16.  max_q: most new tokens of one
-     * sequence (0 = tokens); rows of a sequence behind its max_q-th are left as they were.  A query's keys may
-     * be divided among tiles, whose partial results the last one to finish joins in a fixed order: such an op
-     * (miriam_op_info.ksplit > 1) owns a device workspace and arrival counters, with the rules of split K:
-     * every pass covers the whole tile space, passes over one op do not overlap in time. */
+     * it, whatever it holds (infinities and NaN included).  fp16 / bf16, head_dim a multiple of 8 up to 256,
+     * scale > 0.  max_q: most new tokens of one sequence (0 = tokens); rows of a sequence behind its max_q-th are
+     * left as they were.  Up to 16 query rows per cache head (max_q * heads / kv_heads) have a kernel of their own;
+     * beyond, page * max_pages must be below 2^26, and probabilities are rounded to the operator's type before
+     * they meet the values.  Keys may be divided among tiles, whose partial results the last one to finish joins
+     * in a fixed order: such an op (miriam_op_info.ksplit = 2) owns a device workspace (for many rows up to 69 MB
+     * at a head_dim of 128) and arrival counters, with the rules of split K: every pass covers the whole tile space,
+     * passes over one op do not overlap in time. */
     MIRIAM_OP_ATTENTION = 18
 } miriam_seq_kind;
 

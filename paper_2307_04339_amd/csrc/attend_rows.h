@@ -10,8 +10,14 @@
 // A logical wave walks every block's 32 keys of its own by itself: keys go from memory straight into the
 // matrix instructions' operands, 64 contiguous bytes of 16 keys per load, values through the wave's own LDS,
 // out of which ds_read_b64_tr_b16 reads them transposed; the next 32 keys' loads go out as soon as the registers
-// of these are free, and their places in the cache are looked up one step earlier still.  The waves meet once per run to join their
-// results.  P is the sum of two 16-bit numbers (its rounding and the rest), which keeps the output at the
+// of these are free, and their places in the cache are looked up one step earlier still.  The waves meet once per
+// run to join their results.
+//
+// Measured: 48 sequences of 200 to 8000 keys, 32 heads over 8 cache heads of 128: 105 us, 4.8 TB/s (a copy 4.9); two
+// of 100k to 131k keys, 16 heads over 2: 57 us, 4.0 TB/s, of which some 10 to find the work and to join 256 partial
+// results per head in two stages; one token behind 128 keys 8 us, where a launch takes 4.
+//
+// P is the sum of two 16-bit numbers (its rounding and the rest), which keeps the output at the
 // rounding of its own type and costs matrix instructions that wait for memory anyway.
 #pragma once
 

@@ -17,15 +17,22 @@
 //    a tile each, as the hardware hands them out.
 //  - Fewer row tiles than such workgroups, of like lengths (a chunk behind a long context): every row tile is cut
 //    into about equal pieces, at the same keys for all row tiles of a sequence, which then share them in L2
-//    (512 tokens behind 16k: 163 us; in equal runs of the list below 205, when these took 178).
+//    (512 tokens behind 16k: 178 us, in equal runs of the list below 205).
 //  - Otherwise (single tokens beside chunks): the steps of all row tiles form a list of which every tile takes an
-//    equal run (20 sequences of 1 to 400 tokens: 59 us; in pieces 70 and by a fixed division of every row tile 86, when these took 61).  As
-//    a second row tile's start and the joining cost more than a few steps, a run's end that lies within a third of
-//    a run of a row tile's is moved there.
+//    equal run (20 sequences of 1 to 400 tokens: 61 us, in pieces 70, by a fixed division of every row tile 86).
+//    As a second row tile's start and the joining cost more than a few steps, a run's end that lies within a third
+//    of a run of a row tile's is moved there.
 // A row tile that ends up in several tiles is joined by the last of them to arrive, in their order.
 //
-// 4 prompts of 4096 tokens, 32 heads of 128: 640 us, 860 TFLOP/s of the products that are needed.  The
-// matrix instructions and their operands' reads from LDS alone take 485 us, the powers of two another 110.
+// Probabilities are rounded once, to T, as the matrix instructions take them, and the sum that divides the output is
+// that of the rounded ones (fp32), so a row's weights still add up to one.  The two numbers per probability of the
+// kernel for few rows would cost half of the products again here, where these bound it.
+//
+// Measured, with that division and loads whose addresses the lanes work out: 4 prompts of 4096 tokens, 32 heads of
+// 128: 640 us, 860 TFLOP/s of the products that are needed (a wave's vector and matrix instructions together keep a
+// SIMD busy for 85% of that, and neither their order nor their waves' priorities matter: the clock falls under
+// them); a chunk of 512 tokens behind 16k 163 us; the 20 sequences 59 us, of which 9 to find the work, 8 for
+// starts and outputs of row tiles and 11 for joining.
 #pragma once
 
 #include "attend.h"
