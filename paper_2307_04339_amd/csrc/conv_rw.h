@@ -143,8 +143,16 @@ __global__ __launch_bounds__(kWave * P, (RwKernel<T, C, P>::WAVES_PER_SIMD)) voi
                         for (int e = 0; e < MF::NACC; ++e) {
                             const int dx = (e / 4) * 8 + (e % 4);
                             const float v = acc[sl][i][e] * esc[rd] + esh[rd];
-                            if constexpr (ACT < 0) cb[dx * LDC] = v;
-                            else yb[dx * LDY] = TypeOps<T>::from_f(act_t<T, ACT>(v));
+                            if constexpr (ACT < 0) {
+                                cb[dx * LDC] = v;
+                            } else {
+                                // (fp16: held in 32 bits first.  The compiler makes one instruction of the affine sum
+                                // and its rounding otherwise, for nearly all of a tile's values, which ones depending
+                                // on the block, and the two ways differ by a step in one of some 10^5 values.)
+                                float o = act_t<T, ACT>(v);
+                                if constexpr (__is_same(T, half_t)) asm("" : "+v"(o));
+                                yb[dx * LDY] = TypeOps<T>::from_f(o);
+                            }
                         }
                     }
                 }
