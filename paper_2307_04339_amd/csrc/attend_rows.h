@@ -79,20 +79,12 @@ __global__ __launch_bounds__(kWave * P, DP > 128 ? 1 : 2) void attend_rows_kerne
         if (base + lane < seqs) view = seq_view(a, base + lane);
         blocks = blocks_of(view);
     };
-    auto upto_lane = [&](int n) {  // the sum over the lanes up to and with this one
-#pragma unroll
-        for (int o = 1; o < kWave; o <<= 1) {
-            const int v = __shfl_up(n, o);
-            n += lane >= o ? v : 0;
-        }
-        return n;
-    };
     // All blocks, and each tile's share.  While there are tiles enough for runs of two blocks that do not cross
     // from one head into the next, these are taken (a head's list then counts as even): two blocks take little
     // longer than one, and most heads of short sequences need no joining.
     int total = 0, share = 0, ahead = 0;  // ahead: places up to and with the lane's part of the sequences
     bool even = false;
-    const int per = (seqs + kWave - 1) / kWave;  // sequences of a lane's part (300 of 300 keys, one cache head: 49 us, 64 after 64: 61)
+    const int per = (seqs + kWave - 1) / kWave;  // sequences of a lane's part (300 of 300 keys, one cache head: 40 us, 64 after 64: 61)
     if (a.splits > 1) {
         int sum = 0, pairs = 0;
         if (per == 1) {
@@ -106,21 +98,16 @@ __global__ __launch_bounds__(kWave * P, DP > 128 ? 1 : 2) void attend_rows_kerne
                 pairs += (n + 1) / 2;
             }
         }
-        int all = sum, all_pairs = pairs;
-        for (int o = 32; o > 0; o >>= 1) {
-            all += __shfl_xor(all, o);
-            all_pairs += __shfl_xor(all_pairs, o);
-        }
-        total = __builtin_amdgcn_readfirstlane(all) * heads;
-        all_pairs = __builtin_amdgcn_readfirstlane(all_pairs) * heads;
+        const int all_pairs = all_sum(pairs) * heads;
+        total = all_sum(sum) * heads;
         even = all_pairs <= (int)a.T;
         if (even) total = 2 * all_pairs;
         share = even ? 2 : (total + (int)a.T - 1) / (int)a.T;
-        ahead = upto_lane((even ? 2 * pairs : sum) * heads);
+        ahead = upto_sum((even ? 2 * pairs : sum) * heads);
     }
     auto list = [&]() {
         mine = (even ? (blocks + 1) & ~1 : blocks) * heads;
-        upto = upto_lane(mine);
+        upto = upto_sum(mine);
     };
     auto view_of = [&](int i) {  // of the 64's i-th
         SeqView v;

@@ -31,7 +31,7 @@
 // Measured, with that division and loads whose addresses the lanes work out: 4 prompts of 4096 tokens, 32 heads of
 // 128: 640 us, 860 TFLOP/s of the products that are needed (a wave's vector and matrix instructions together keep a
 // SIMD busy for 85% of that, and neither their order nor their waves' priorities matter: the clock falls under
-// them); a chunk of 512 tokens behind 16k 163 us; the 20 sequences 59 us, of which 9 to find the work, 8 for
+// them); a chunk of 512 tokens behind 16k 161 us; the 20 sequences 57 us, of which 5 to find the work, 8 for
 // starts and outputs of row tiles and 11 for joining.
 #pragma once
 
@@ -125,17 +125,9 @@ __global__ __launch_bounds__(kWave * P, DP > 128 ? 1 : 2) void attend_tile_kerne
     auto steps = [&](const Span &p) {  // one where there are no keys, to write the rows' zeros
         return p.end > p.begin ? (p.end + kTileKeys - 1) / kTileKeys - p.begin / kTileKeys : 1;
     };
-    auto scan = [&](int n) {
-#pragma unroll
-        for (int o = 1; o < kWave; o <<= 1) {
-            const int v = __shfl_up(n, o);
-            n += lane >= o ? v : 0;
-        }
-        return n;
-    };
     // row tiles of a cache head, the longest sequence's steps, and at least half of all; a lane goes through its part
     // of the sequences, so that a tile need not look through all of them again (1000 sequences of 128 tokens, 12
-    // heads of 64: 446 us, 64 sequences after 64 twice 581)
+    // heads of 64: 430 us, 64 sequences after 64 twice 581)
     const int per = (seqs + kWave - 1) / kWave;
     int J = 0, longest = 0;
     float half = 0.0f;
@@ -153,16 +145,11 @@ __global__ __launch_bounds__(kWave * P, DP > 128 ? 1 : 2) void attend_tile_kerne
         } else {
             for (int s = lane * per; s < (lane + 1) * per && s < seqs; ++s) add(seq_view(a, s));
         }
-        const int ahead = scan(J);  // row tiles up to and with the lane's part
+        const int ahead = upto_sum(J);  // row tiles up to and with the lane's part
         if (pw == 0) s_ahead[lane] = ahead;
         J = __builtin_amdgcn_readlane(ahead, kWave - 1);
-#pragma unroll
-        for (int o = 32; o > 0; o >>= 1) {
-            const int v = __shfl_xor(longest, o);
-            longest = longest > v ? longest : v;
-            half += __shfl_xor(half, o);
-        }
-        longest = __builtin_amdgcn_readfirstlane(longest);
+        longest = all_max(longest);
+        half = all_sum(half);
         __syncthreads();
     }
     // where to look for row tile j: the first sequence of its part, and the row tiles before that
@@ -185,7 +172,7 @@ __global__ __launch_bounds__(kWave * P, DP > 128 ? 1 : 2) void attend_tile_kerne
         int from, before;
         for (part_of(c * kWave, from, before); from < seqs; from += kWave) {
             look(from);
-            const int upto = scan(ntiles), all = __builtin_amdgcn_readlane(upto, kWave - 1);
+            const int upto = upto_sum(ntiles), all = __builtin_amdgcn_readlane(upto, kWave - 1);
             int i = 0;  // sequences of these that end at or before it
 #pragma unroll
             for (int o = kWave / 2; o > 0; o >>= 1) i += __shfl(upto, i + o - 1) <= want - before ? o : 0;
@@ -225,15 +212,8 @@ __global__ __launch_bounds__(kWave * P, DP > 128 ? 1 : 2) void attend_tile_kerne
         head_places = biggest = 0;
         for (int c = chunks - 1; c >= 0; --c) {
             get(c);
-            int n = places(ch.n), m = n > 0 ? (ch.n + n - 1) / n : 0;
-#pragma unroll
-            for (int o = 32; o > 0; o >>= 1) {
-                const int v = __shfl_xor(m, o);
-                m = v > m ? v : m;
-                n += __shfl_xor(n, o);
-            }
-            head_places += __builtin_amdgcn_readfirstlane(n);
-            m = __builtin_amdgcn_readfirstlane(m);
+            const int n = places(ch.n), m = all_max(n > 0 ? (ch.n + n - 1) / n : 0);
+            head_places += all_sum(n);
             biggest = biggest > m ? biggest : m;
         }
     };
@@ -283,7 +263,7 @@ __global__ __launch_bounds__(kWave * P, DP > 128 ? 1 : 2) void attend_tile_kerne
         if (list) {
             for (int c = 0; c < chunks && s < 0; ++c) {
                 get(c);
-                const int upto = scan(places(ch.n)), here = __builtin_amdgcn_readlane(upto, kWave - 1);
+                const int upto = upto_sum(places(ch.n)), here = __builtin_amdgcn_readlane(upto, kWave - 1);
                 if (inside < here) {
                     const int i = __builtin_popcountll(__ballot(upto <= inside));
                     inside -= i > 0 ? __builtin_amdgcn_readlane(upto, i - 1) : 0;
@@ -299,7 +279,7 @@ __global__ __launch_bounds__(kWave * P, DP > 128 ? 1 : 2) void attend_tile_kerne
             int from, before;
             for (part_of(j, from, before); from < seqs && s < 0; from += kWave) {
                 look(from);
-                const int upto = scan(ntiles), all = __builtin_amdgcn_readlane(upto, kWave - 1);
+                const int upto = upto_sum(ntiles), all = __builtin_amdgcn_readlane(upto, kWave - 1);
                 if (j - before < all) {
                     const int i = __builtin_popcountll(__ballot(upto <= j - before));
                     s = from + i;

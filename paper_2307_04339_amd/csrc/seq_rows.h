@@ -12,6 +12,31 @@ __device__ __forceinline__ int seq_len(const SeqArgs &q, int64_t s) {
     return clampi(q.kv_len[s], 0, q.table ? q.page * q.max_pages : 0x3fffffff);
 }
 
+// f over the values of the lanes up to and with this one, 0 being neutral to it; six data-parallel moves.
+template <class T, class F>
+__device__ __forceinline__ T upto_lane(T v, F f) {
+    auto from = [&](auto ctrl, auto rows) {
+        return __builtin_bit_cast(T, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), decltype(ctrl)::value, decltype(rows)::value, 0xf, false));
+    };
+    v = f(v, from(ActTag<0x111>{}, ActTag<0xf>{}));  // 1, 2, 4 and 8 lanes back in each row of 16
+    v = f(v, from(ActTag<0x112>{}, ActTag<0xf>{}));
+    v = f(v, from(ActTag<0x114>{}, ActTag<0xf>{}));
+    v = f(v, from(ActTag<0x118>{}, ActTag<0xf>{}));
+    v = f(v, from(ActTag<0x142>{}, ActTag<0xa>{}));  // the last lane of rows 0 and 2 to rows 1 and 3
+    v = f(v, from(ActTag<0x143>{}, ActTag<0xc>{}));  // lane 31 to rows 2 and 3
+    return v;
+}
+__device__ __forceinline__ int upto_sum(int v) {
+    return upto_lane(v, [](int a, int b) { return a + b; });
+}
+__device__ __forceinline__ int all_sum(int v) { return __builtin_amdgcn_readlane(upto_sum(v), kWave - 1); }
+__device__ __forceinline__ int all_max(int v) {  // of values >= 0
+    return __builtin_amdgcn_readlane(upto_lane(v, [](int a, int b) { return a > b ? a : b; }), kWave - 1);
+}
+__device__ __forceinline__ float all_sum(float v) {
+    return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, upto_lane(v, [](float a, float b) { return a + b; })), kWave - 1));
+}
+
 // Loads and stores past the caches.  (The empty statements keep the compiler from merging them with ordinary ones in
 // the other branch of a condition, which makes both ordinary.)
 template <class T>
