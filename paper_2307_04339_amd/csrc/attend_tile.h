@@ -17,9 +17,9 @@
 //    a tile each, as the hardware hands them out.
 //  - Fewer row tiles than such workgroups, of like lengths (a chunk behind a long context): every row tile is cut
 //    into about equal pieces, at the same keys for all row tiles of a sequence, which then share them in L2
-//    (512 tokens behind 16k: 178 us, in equal runs of the list below 205).
+//    (512 tokens behind 16k: 178 us then, in equal runs of the list below 205).
 //  - Otherwise (single tokens beside chunks): the steps of all row tiles form a list of which every tile takes an
-//    equal run (20 sequences of 1 to 400 tokens: 61 us, in pieces 70, by a fixed division of every row tile 86).
+//    equal run (20 sequences of 1 to 400 tokens: 61 us then, in pieces 70, by a fixed division of every row tile 86).
 //    As a second row tile's start and the joining cost more than a few steps, a run's end that lies within a third
 //    of a run of a row tile's is moved there.
 // A row tile that ends up in several tiles is joined by the last of them to arrive, in their order.
@@ -31,7 +31,7 @@
 // Measured, with that division and loads whose addresses the lanes work out: 4 prompts of 4096 tokens, 32 heads of
 // 128: 640 us, 860 TFLOP/s of the products that are needed (a wave's vector and matrix instructions together keep a
 // SIMD busy for 85% of that, and neither their order nor their waves' priorities matter: the clock falls under
-// them); a chunk of 512 tokens behind 16k 161 us; the 20 sequences 57 us, of which 5 to find the work, 8 for
+// them); a chunk of 512 tokens behind 16k 161 us; the 20 sequences (heads of 80) 53 us, of which 5 to find the work, 8 for
 // starts and outputs of row tiles and 11 for joining.
 #pragma once
 
@@ -40,10 +40,12 @@
 
 namespace miriam {
 
-template <class T, int DP, int P>
+// DP: a row in LDS; DE: values of it that the products take, as many 32s as a head has (heads of 80, the 20 sequences
+// above: 53 us with 96, 57 with 128).
+template <class T, int DP, int P, int DE>
 struct TileKernel {
-    static constexpr int NJ = DP / 16;        // 16-value steps of a key
-    static constexpr int ND = DP / 32;        // 32-value tiles of the output
+    static constexpr int NJ = DE / 16;        // 16-value steps of a key
+    static constexpr int ND = DE / 32;        // 32-value tiles of the output
     static constexpr int CPR = DP / 8;        // 16-byte pieces of a row
     static constexpr int RPL = kWave / CPR;   // rows per load
     static constexpr int NLD = kTileKeys / RPL;  // loads per stage of keys (and of values)
@@ -58,9 +60,9 @@ struct TileKernel {
     static constexpr __device__ int vswz(int r) { return DP == 64 ? ((r >> 1) & 1) << 2 : (r & 3) << 2; }
 };
 
-template <class T, int DP, int P, bool UNI>
+template <class T, int DP, int P, bool UNI, int DE>
 __global__ __launch_bounds__(kWave * P, DP > 128 ? 1 : 2) void attend_tile_kernel(AttendArgs a, Shard sh) {
-    typedef TileKernel<T, DP, P> K_;
+    typedef TileKernel<T, DP, P, DE> K_;
     typedef Mfma<T, 32> MF;
     typedef typename MF::op_t op_t;
     typedef typename MF::acc_t acc_t;
@@ -760,18 +762,18 @@ __global__ __launch_bounds__(kWave * P, DP > 128 ? 1 : 2) void attend_tile_kerne
     }
 }
 
-template <class T, int DP, bool UNI>
+template <class T, int DP, bool UNI, int DE>
 inline void tile_table_u(const void *out[3], int *lds) {
-    out[0] = reinterpret_cast<const void *>(&attend_tile_kernel<T, DP, 1, UNI>);
-    out[1] = reinterpret_cast<const void *>(&attend_tile_kernel<T, DP, 2, UNI>);
-    out[2] = reinterpret_cast<const void *>(&attend_tile_kernel<T, DP, 4, UNI>);
-    *lds = TileKernel<T, DP, 4>::LDS_BYTES;
+    out[0] = reinterpret_cast<const void *>(&attend_tile_kernel<T, DP, 1, UNI, DE>);
+    out[1] = reinterpret_cast<const void *>(&attend_tile_kernel<T, DP, 2, UNI, DE>);
+    out[2] = reinterpret_cast<const void *>(&attend_tile_kernel<T, DP, 4, UNI, DE>);
+    *lds = TileKernel<T, DP, 4, DE>::LDS_BYTES;
 }
 // uni: a load's 512 / dp rows lie in one page (the page a multiple of them) and span less than 2^31 bytes
-template <class T, int DP>
+template <class T, int DP, int DE = DP>
 inline void tile_table(bool uni, const void *out[3], int *lds) {
-    if (uni) tile_table_u<T, DP, true>(out, lds);
-    else tile_table_u<T, DP, false>(out, lds);
+    if (uni) tile_table_u<T, DP, true, DE>(out, lds);
+    else tile_table_u<T, DP, false, DE>(out, lds);
 }
 
 }  // namespace miriam

@@ -48,8 +48,8 @@ int rotary_kernels(int dtype, bool vec, const void *out[3]);
 // attention, head_dim <= dp in {64, 128, 256}: up to 16 query rows per cache head, or tiles of 128
 int attend_rows_kernels_f16(int dp, const void *out[3], int *lds);
 int attend_rows_kernels_bf16(int dp, const void *out[3], int *lds);
-int attend_tile_kernels_f16(int dp, bool uni, const void *out[3], int *lds);
-int attend_tile_kernels_bf16(int dp, bool uni, const void *out[3], int *lds);
+int attend_tile_kernels_f16(int d, bool uni, const void *out[3], int *lds);
+int attend_tile_kernels_bf16(int d, bool uni, const void *out[3], int *lds);
 int rw_kernels(int dtype, int64_t ks, int64_t stride, int64_t c, const void *out[3], int *lds);
 
 }  // namespace miriam

@@ -277,7 +277,7 @@ static int create_attention(miriam_op *op) {
     // many rows: the rows of one load (512 / dp keys) always in one page
     const bool f16 = d.dtype == MIRIAM_F16, uni = d.page % (512 / dp) == 0 && d.cache_token < ((int64_t)1 << 26);
     if ((rows ? (f16 ? attend_rows_kernels_f16(dp, op->kern, &op->lds_bytes) : attend_rows_kernels_bf16(dp, op->kern, &op->lds_bytes))
-              : (f16 ? attend_tile_kernels_f16(dp, uni, op->kern, &op->lds_bytes) : attend_tile_kernels_bf16(dp, uni, op->kern, &op->lds_bytes))) != 0)
+              : (f16 ? attend_tile_kernels_f16(a.d, uni, op->kern, &op->lds_bytes) : attend_tile_kernels_bf16(a.d, uni, op->kern, &op->lds_bytes))) != 0)
         return einval("attention: no kernel for this dtype");
     // at full capacity
     op->flops = 4.0 * (double)d.tokens * (double)width * (double)keys;

@@ -340,6 +340,8 @@ DIVISIONS = [
     ([2100], [2100], 32, 32, 64, 64, False, 0, None),                                      # a tile for each
     ([1] * 200, [1 + 11 * i % 700 for i in range(200)], 8, 4, 64, 16, False, 0, 1),        # single tokens of many sequences
     ([1, 1, 1], [40000, 3, 129], 2, 1, 128, 64, False, 0, 1),                              # joined in two stages
+    ([1, 300, 1, 77, 1, 1], [3000, 700, 50, 4000, 1, 2047], 10, 5, 80, 24, True, 1500, None),  # heads of whole 32s but the last
+    ([513], [9000], 4, 1, 96, 18, False, 0, None),                                         # pages that no load divides
     # several sequences to a lane that looks for a tile's work
     ([i % 50 for i in range(200)], [i % 50 + 3 * i % 90 for i in range(200)], 16, 4, 64, 16, False, 0, None),
     ([0] * 90 + [30, 1] + [0] * 60 + [7] * 3, [5] * 90 + [2500, 40] + [0] * 60 + [700, 7, 1300], 8, 2, 64, 16, False, 0, None),
