@@ -69,6 +69,23 @@ static Rows cache_span(const miriam_seq_desc &d, const void *p, int es) {
     return {p, 1, n, n, es};
 }
 
+// Whether all places of two caches of the same strides, `apart` elements from one to the other, are of their own: of
+// the dimensions with more than one entry, the caches themselves among them, each must step past all that the ones of
+// shorter steps reach.  (So caches may lie one behind the other, or interleaved at any level.)
+static bool own_places(const miriam_seq_desc &d, int64_t apart) {
+    struct Dim {
+        int64_t step, n;
+    } dims[4] = {{d.cache_page, d.pages}, {d.cache_head, d.kv_heads}, {d.cache_token, d.page}, {apart, 2}};
+    std::sort(dims, dims + 4, [](const Dim &a, const Dim &b) { return a.step < b.step; });
+    int64_t reach = d.head_dim;
+    for (const Dim &m : dims) {
+        if (m.n < 2) continue;
+        if (m.step < reach) return false;
+        reach += (m.n - 1) * m.step;
+    }
+    return true;
+}
+
 // The heads of a descriptor.
 static int check_heads(const miriam_seq_desc &d) {
     if (d.heads < 1 || d.kv_heads < 0 || d.head_dim < 1 || d.heads >= kMost || d.kv_heads >= kMost || d.head_dim >= kMost ||
@@ -165,6 +182,10 @@ static int create_rotary(miriam_op *op) {
     if (d.kv_heads > 0) {
         const Rows k = cache_span(d, a.k, es), v = cache_span(d, a.v, es);
         if (a.k == a.v) return einval("rotary: both caches are one");
+        // (two stores to one place would leave either)
+        const uintptr_t ka = (uintptr_t)a.k, va = (uintptr_t)a.v, bytes = ka < va ? va - ka : ka - va;
+        if (!own_places(d, (int64_t)std::min<uintptr_t>(bytes / (uintptr_t)es, (uintptr_t)1 << 62)))
+            return einval("rotary: places of the caches overlap (each stride must step past what the shorter ones reach)");
         if (overlap(x, k) || overlap(x, v) || overlap(y, k) || overlap(y, v)) return einval("rotary: x or y overlaps a cache");
     }
     a.heads = (int32_t)d.heads; a.kv_heads = (int32_t)d.kv_heads; a.d = (int32_t)d.head_dim; a.rot = (int32_t)d.rot;

@@ -1,0 +1,73 @@
+"""Stores of the operators over packed token rows that would meet are refused at creation (no GPU needed)."""
+import itertools
+
+import numpy as np
+import pytest
+
+from test_seq_ops import ATT, ROT, L, _at, _create  # noqa: F401  (L: fixture)
+
+ES = 2
+PAGES, KV, PAGE, D = 8, 2, 16, 64        # of ROT and ATT
+
+
+def _refused(L, base, changes):
+    rc, h = _create(L, **dict(base, **changes))
+    assert rc == L.EINVAL and h.value is None, changes
+    return L.load().miriam_last_error()
+
+
+def _accepted(L, base, changes):
+    rc, h = _create(L, **dict(base, **changes))
+    assert rc == 0, (changes, L.load().miriam_last_error())
+    L.load().miriam_op_destroy(h)
+
+
+# ----------------------------------------------------- places of the two caches
+@pytest.mark.parametrize("changes", [
+    dict(v_cache=_at(3) + 8 * ES),                                   # v a few values behind k
+    dict(v_cache=_at(3) + 2048 * ES),                                # a page behind it: its pages are k's next ones
+    dict(v_cache=_at(3) - 2048 * ES),
+    dict(v_cache=_at(3) + 1024 * ES, cache_page=4096),               # values of head 0 where the keys of head 1 lie
+    dict(cache_head=8), dict(cache_page=64),                         # heads, pages that overlap
+    dict(cache_head=64, cache_token=64),
+    dict(cache_page=1024, cache_head=2048),                          # pages within the heads' steps, but longer than theirs
+    dict(v_cache=_at(3) + 64 * ES, cache_token=96, cache_head=1536, cache_page=3072),   # interleaved, tokens too near
+])
+def test_caches_whose_places_overlap_are_refused(L, changes):  # noqa: F811
+    assert b"overlap" in _refused(L, ROT, changes)
+
+
+@pytest.mark.parametrize("changes", [
+    dict(v_cache=_at(3) + PAGES * 2048 * ES),                        # one behind the other
+    dict(v_cache=_at(3) - PAGES * 2048 * ES),
+    dict(v_cache=_at(3) + 2048 * ES, cache_page=4096),               # keys and values of a page in turn
+    dict(v_cache=_at(3) + 1024 * ES, cache_page=4096, cache_head=2048),                  # of a head
+    dict(v_cache=_at(3) + 64 * ES, cache_token=128, cache_head=2048, cache_page=4096),   # of a token
+    dict(v_cache=_at(3) + 128 * ES, cache_token=256, cache_head=64, cache_page=4096),    # of a token's heads
+    dict(cache_token=128, cache_head=64),                            # a token's heads together
+    dict(cache_page=64, cache_token=512, cache_head=512 * 16),       # pages innermost
+    dict(kv_heads=1, cache_head=1), dict(pages=1, cache_page=1),     # steps that nothing takes
+])
+def test_caches_of_their_own_places_are_accepted(L, changes):  # noqa: F811
+    _accepted(L, ROT, changes)
+
+
+def test_what_is_accepted_has_places_of_its_own(L):  # noqa: F811
+    """Every accepted combination of small strides, place by place."""
+    pages, kv, page, d = 3, 2, 2, 2
+    base = dict(ROT, pages=pages, kv_heads=kv, page=page, head_dim=d, rot=2, heads=2)
+    grid = np.array(list(itertools.product(range(pages), range(kv), range(page))))
+    taken = 0
+    for sp, sh, st in itertools.product((2, 3, 4, 6, 8, 12), repeat=3):
+        for apart in (2, 4, 6, 8, 12, 24, 64):
+            rc, h = _create(L, **dict(base, cache_page=sp, cache_head=sh, cache_token=st, v_cache=_at(3) + apart * ES))
+            at = (grid @ np.array([sp, sh, st]))[:, None] + np.arange(d)
+            both = np.concatenate([at, at + apart]).ravel()
+            if rc == 0:
+                taken += 1
+                assert len(set(both)) == len(both), (sp, sh, st, apart)
+                L.load().miriam_op_destroy(h)
+            # (what a contiguous allocation gives is accepted)
+            elif len(set(both)) == len(both):
+                assert max(both) + 1 > len(both), (sp, sh, st, apart)
+    assert taken > 10
