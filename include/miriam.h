@@ -281,9 +281,10 @@ int miriam_op_destroy(miriam_op *op);
  * the work follows from them.
  *
  * The coordinator runs an operator several times when it measures it, so none of these works in place: an
- * output that overlaps rows, weights or caches that are read is refused (columns of their own in rows of one
- * buffer are no overlap).  ROTARY wants two caches all of whose places are their own: the caches may be interleaved, but
- * of pages, heads, tokens and the two caches each must step past all that the ones of shorter steps reach.
+ * output (for ROTARY the caches, too) that overlaps rows, weights, caches, frequencies or the batch's arrays that
+ * are read is refused (columns of their own in rows of one buffer are no overlap).  ROTARY wants two caches all of
+ * whose places are their own: they may be interleaved, but of pages, heads, tokens and the two caches each must
+ * step past all that the ones of shorter steps reach.
  */
 typedef enum {
     /* Norms around a block, with its gate and residual, over rows of n values:

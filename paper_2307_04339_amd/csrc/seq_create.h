@@ -46,7 +46,7 @@ static int check_seqs(const miriam_seq_desc &d, SeqArgs &q, bool cache) {
         d.page * d.max_pages >= kMost)
         return einval("page, pages and max_pages must be >= 1, and page * max_pages below 2^30");
     q.ldt = d.ldt > 0 ? d.ldt : d.max_pages;
-    if (q.ldt < d.max_pages) return einval("page table: row stride too small");
+    if (q.ldt < d.max_pages || q.ldt > ((int64_t)1 << 58) / d.seqs) return einval("page table: row stride too small or too large");
     if (d.cache_page < 1 || d.cache_head < 1 || d.cache_token < 1) return einval("cache strides must be >= 1");
     if (d.page > 1 && d.cache_token < d.head_dim) return einval("cache: token stride smaller than a head");
     constexpr int64_t far = (int64_t)1 << 58;  // bytes of a cache stay below 2^62
@@ -67,6 +67,12 @@ static int check_seqs(const miriam_seq_desc &d, SeqArgs &q, bool cache) {
 static Rows cache_span(const miriam_seq_desc &d, const void *p, int es) {
     const int64_t n = (d.pages - 1) * d.cache_page + (d.kv_heads - 1) * d.cache_head + (d.page - 1) * d.cache_token + d.head_dim;
     return {p, 1, n, n, es};
+}
+
+// Whether rows that are stored share memory with the arrays of the batch.
+static bool over_batch(const miriam_seq_desc &d, const SeqArgs &q, const Rows &out) {
+    return overlap({q.q_start, 1, q.seqs + 1, q.seqs + 1, 4}, out) || overlap({q.kv_len, 1, q.seqs, q.seqs, 4}, out) ||
+           overlap({q.table, q.seqs, d.max_pages, q.ldt, 4}, out);
 }
 
 // Whether all places of two caches of the same strides, `apart` elements from one to the other, are of their own: of
@@ -178,7 +184,9 @@ static int create_rotary(miriam_op *op) {
     for (const void *p : {a.x, (const void *)a.y, (const void *)a.k, (const void *)a.v})
         if (!aligned(p, (uintptr_t)es)) return einval("rotary: x, y and the caches must be aligned to their type");
     const Rows x{a.x, d.tokens, width, a.ldx, es}, y{a.y, d.tokens, d.heads * d.head_dim, a.ldy, es};
+    const Rows freq{d.rot > 0 ? a.freq : nullptr, 1, d.rot / 2, d.rot / 2, 8};
     if (overlap(x, y)) return einval("rotary: y overlaps x");
+    if (over_batch(d, a.sq, y) || overlap(freq, y)) return einval("rotary: y overlaps q_start, kv_len, page_table or freq");
     if (d.kv_heads > 0) {
         const Rows k = cache_span(d, a.k, es), v = cache_span(d, a.v, es);
         if (a.k == a.v) return einval("rotary: both caches are one");
@@ -187,6 +195,8 @@ static int create_rotary(miriam_op *op) {
         if (!own_places(d, (int64_t)std::min<uintptr_t>(bytes / (uintptr_t)es, (uintptr_t)1 << 62)))
             return einval("rotary: places of the caches overlap (each stride must step past what the shorter ones reach)");
         if (overlap(x, k) || overlap(x, v) || overlap(y, k) || overlap(y, v)) return einval("rotary: x or y overlaps a cache");
+        for (const Rows &c : {k, v})
+            if (over_batch(d, a.sq, c) || overlap(freq, c)) return einval("rotary: a cache overlaps q_start, kv_len, page_table or freq");
     }
     a.heads = (int32_t)d.heads; a.kv_heads = (int32_t)d.kv_heads; a.d = (int32_t)d.head_dim; a.rot = (int32_t)d.rot;
     a.interleaved = (d.flags & MIRIAM_SEQ_INTERLEAVED) ? 1 : 0;
@@ -241,6 +251,7 @@ static int create_attention(miriam_op *op) {
     const Rows y{a.y, d.tokens, width, a.ldy, 2};
     if (overlap({a.x, d.tokens, width, a.ldx, 2}, y)) return einval("attention: y overlaps x");
     if (overlap(y, cache_span(d, a.k, 2)) || overlap(y, cache_span(d, a.v, 2))) return einval("attention: y overlaps a cache");
+    if (over_batch(d, a.sq, y)) return einval("attention: y overlaps q_start, kv_len or page_table");
     a.heads = (int32_t)d.heads; a.kv_heads = (int32_t)d.kv_heads; a.group = (int32_t)(d.heads / d.kv_heads); a.d = (int32_t)d.head_dim;
     a.fd_group = make_fastdiv((uint32_t)a.group);
     a.fd_kv = make_fastdiv((uint32_t)a.kv_heads);

@@ -71,3 +71,36 @@ def test_what_is_accepted_has_places_of_its_own(L):  # noqa: F811
             elif len(set(both)) == len(both):
                 assert max(both) + 1 > len(both), (sp, sh, st, apart)
     assert taken > 10
+
+
+# --------------------------------------------- outputs over what a pass reads
+OUT = 10 * 4 * 64 * ES                   # bytes of y in ROT and ATT
+CACHE = PAGES * 2048 * ES                # and of a cache
+
+
+@pytest.mark.parametrize("array,size", [("q_start", 12), ("kv_len", 8), ("page_table", 2 * 4 * 4)])
+@pytest.mark.parametrize("base,out,reach", [(ROT, "y", OUT), (ROT, "k_cache", CACHE), (ROT, "v_cache", CACHE), (ATT, "y", OUT)])
+def test_outputs_over_the_batchs_arrays_are_refused(L, base, out, reach, array, size):  # noqa: F811
+    at = base[out]
+    for start in (at, at + reach - 4, at - size + 4):
+        _refused(L, base, {array: start})
+    for start in (at + reach, at - size):                            # right behind it, and right before
+        _accepted(L, base, {array: start})
+
+
+@pytest.mark.parametrize("out,reach", [("y", OUT), ("k_cache", CACHE), ("v_cache", CACHE)])
+def test_outputs_over_the_frequencies_are_refused(L, out, reach):  # noqa: F811
+    at, size = ROT[out], 32 * 8
+    for start in (at, at + reach - 8, at - size + 8):
+        _refused(L, ROT, dict(freq=start))
+    for start in (at + reach, at - size):
+        _accepted(L, ROT, dict(freq=start))
+    _accepted(L, ROT, dict(freq=at, rot=0))                          # nothing is turned, nothing is read
+
+
+def test_strided_outputs_and_tables(L):  # noqa: F811
+    _refused(L, ATT, dict(page_table=_at(2) + 9 * 512 * ES, ldy=512))       # in the last row of a strided y
+    _refused(L, ATT, dict(page_table=_at(2) - 400, ldt=100))                # the table's second row
+    _refused(L, ATT, dict(ldt=1 << 60))
+    _accepted(L, ATT, dict(kv_len=_at(3), q_start=_at(3), page_table=_at(3)))   # only read: may share memory
+    _accepted(L, dict(ROT, kv_heads=0, k_cache=None, v_cache=None), dict(page_table=_at(2)))   # no cache: no table
