@@ -239,8 +239,8 @@ __global__ __launch_bounds__(kWave * P, DP > 128 ? 1 : 2) void attend_tile_kerne
             near = near > 1 ? near : 1;
         }
     }
-    const int total = head_places * a.kv_heads, run = total / runs, more = total - run * runs;
-    auto start = [&](int k) { return k * run + k * more / runs; };  // floor(k total / runs)
+    const int total = head_places * a.kv_heads;
+    const Runs division = runs_of(total, runs);
 
     int iter = 0;
     for (int64_t t = sh.begin + rank; t < sh.begin + sh.len; t += G, ++iter) {
@@ -251,8 +251,8 @@ __global__ __launch_bounds__(kWave * P, DP > 128 ? 1 : 2) void attend_tile_kerne
         int at = 0, stop = 1, hk, j, s = -1, qi = 0, inside = 0;
         if (list) {
             if (t >= runs) continue;
-            at = start((int)t);
-            stop = start((int)t + 1);
+            at = division.start((int)t);
+            stop = division.start((int)t + 1);
             hk = at / head_places;
             inside = at - hk * head_places;
             j = 0;

@@ -77,6 +77,17 @@ struct AttendArgs {
 constexpr int kRowKeys = 128;    // keys of a block of the kernel for few query rows: 32 for each logical wave
 constexpr int kTileRows = 128;   // query rows of a tile of the kernel for many: 32 for each logical wave
 constexpr int kTileKeys = 64;    // and its keys per step
+// Runs that share a list of places: run k begins at floor(k places / runs).  (Without new tokens there are neither
+// places nor runs, and nothing to divide.)
+struct Runs {
+    int runs, run, more;
+    constexpr int start(int k) const { return k * run + k * more / runs; }
+};
+constexpr Runs runs_of(int places, int runs) {
+    const int run = runs > 0 ? places / runs : 0;
+    return {runs, run, places - run * runs};
+}
+
 // fp32 values of a partial result: rows x (dp values, maximum, sum)
 constexpr int64_t attend_partial(int rows, int dp) { return (int64_t)rows * (dp + 2); }
 
