@@ -305,8 +305,8 @@ typedef enum {
     /* Attention of the new tokens over the paged cache: y = sum_j softmax_j(scale * q . k_j) v_j for every
      * query head, heads / kv_heads consecutive ones sharing a cache head, over the keys j < kv_len[s] that
      * are there and, with MIRIAM_SEQ_CAUSAL, at or before the token's position, and with window > 0 among the
-     * `window` last ones up to it.  A row without keys gives zeros, and what a row does not see never reaches
-     * it, whatever it holds (infinities and NaN included).  fp16 / bf16, head_dim a multiple of 8 up to 256,
+     * `window` last ones up to it.  A row without keys gives zeros, one that sees keys whose scores are all -inf
+     * NaN, and what a row does not see never reaches it, whatever it holds (infinities and NaN included).  fp16 / bf16, head_dim a multiple of 8 up to 256,
      * scale > 0.  max_q: most new tokens of one sequence (0 = tokens); rows of a sequence behind its max_q-th are
      * left as they were.  Up to 16 query rows per cache head (max_q * heads / kv_heads) have a kernel of their own;
      * beyond, page * max_pages must be below 2^26, and probabilities are rounded to the operator's type before

@@ -22,6 +22,9 @@ namespace miriam {
 template <class T> constexpr float kShift = 0.0f;
 template <> inline constexpr float kShift<half_t> = 6.0f;
 constexpr float kRise = 8.0f;
+// The maximum of a row is -inf where it sees no key, and at least this where it does: scores that are all -inf give 0 / 0,
+// as the definition has it, and no keys give zeros.
+constexpr float kLowest = -3.402823466e+38f;
 
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
@@ -56,6 +59,9 @@ __device__ __forceinline__ int64_t key_place(const AttendArgs &a, int64_t s, con
 }
 
 __device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// What a row's sums are multiplied by at last, m being its maximum.
+__device__ __forceinline__ float one_over(float l, float m) { return m == -INFINITY ? 0.0f : 1.0f / l; }
 
 // Two 32-bit floats rounded to T, packed.
 template <class T>

@@ -310,6 +310,7 @@ __global__ __launch_bounds__(kWave * P, DP > 128 ? 1 : 2) void attend_rows_kerne
                     const auto s32 = __builtin_amdgcn_permlane32_swap(w, w, false, false);
                     top = fmaxf(__builtin_bit_cast(float, (uint32_t)s32[0]), __builtin_bit_cast(float, (uint32_t)s32[1]));
                 }
+                if (row_seen) top = fmaxf(top, kLowest);
                 const float m1 = fmaxf(m, top), ms = m1 == -INFINITY ? 0.0f : m1;
                 const float alpha = m == -INFINITY ? 1.0f : exp2_(m - ms);  // (nothing to lower before the first key)
                 m = m1;
@@ -361,10 +362,10 @@ __global__ __launch_bounds__(kWave * P, DP > 128 ? 1 : 2) void attend_rows_kerne
         // ---- the four logical waves' results, in order
         const bool whole = w0 == w1;
         const int slot0 = (int)t * 2 + (t == w0 ? 1 : 0);
-        auto put = [&](int r, int d4, const f32x4 &o, float, float l) {
+        auto put = [&](int r, int d4, const f32x4 &o, float m, float l) {
             const int tok = (int)fdiv((uint32_t)r, a.fd_group);
             T *yr = Y + (int64_t)(sv.q0 + tok) * a.ldy + (int64_t)(hk * g + r - tok * g) * a.d + d4;
-            const float inv = l > 0.0f || l != l ? 1.0f / l : 0.0f;  // no key: zeros
+            const float inv = one_over(l, m);
             u32x2 w;
             w[0] = pack2<T>(o[0] * inv, o[1] * inv);
             w[1] = pack2<T>(o[2] * inv, o[3] * inv);

@@ -472,7 +472,7 @@ __global__ __launch_bounds__(kWave * P, DP > 128 ? 1 : 2) void attend_tile_kerne
                 acc_t s[2];
             };
             u32x4 op[LA + 1], p[2][2];
-            float top, sub;
+            float top, low, sub;  // low: what top is at least, once scaled
             lds_char kst, vst;
             auto read = [&](auto n_) __attribute__((always_inline)) {
                 constexpr int n = decltype(n_)::value;
@@ -510,7 +510,8 @@ __global__ __launch_bounds__(kWave * P, DP > 128 ? 1 : 2) void attend_tile_kerne
             };
             // scores of keys that a row does not see; lane: row xl, key 32 kt + 8 (i / 4) + 4 hx + i % 4
             auto mask = [&](int b, uint64_t there, Scores &z) __attribute__((always_inline)) {
-                const uint64_t w = (there & seen_keys(a, b * kTileKeys, pos)) >> (4 * hx);
+                const uint64_t all = there & seen_keys(a, b * kTileKeys, pos), w = all >> (4 * hx);
+                if (all == 0) low = -INFINITY;
                 const uint32_t seen[2] = {(uint32_t)w, (uint32_t)(w >> 32)};
 #pragma unroll
                 for (int kt = 0; kt < 2; ++kt)
@@ -521,7 +522,7 @@ __global__ __launch_bounds__(kWave * P, DP > 128 ? 1 : 2) void attend_tile_kerne
             auto raise = [&]() __attribute__((always_inline)) {
                 const uint32_t u = __builtin_bit_cast(uint32_t, top);
                 const auto s32 = __builtin_amdgcn_permlane32_swap(u, u, false, false);
-                top = fmaxf(__builtin_bit_cast(float, (uint32_t)s32[0]), __builtin_bit_cast(float, (uint32_t)s32[1])) * a.scale;
+                top = fmaxf(fmaxf(__builtin_bit_cast(float, (uint32_t)s32[0]), __builtin_bit_cast(float, (uint32_t)s32[1])) * a.scale, low);
                 if (__ballot(top > m + kRise)) {  // (-inf: the first key raises it)
                     const float m1 = top > m + kRise ? top : m;
                     const float alpha = m == m1 || m == -INFINITY ? 1.0f : exp2_(m - m1);  // (nothing to lower before the first key)
@@ -550,6 +551,7 @@ __global__ __launch_bounds__(kWave * P, DP > 128 ? 1 : 2) void attend_tile_kerne
                     score(n, zn);
                     __builtin_amdgcn_sched_barrier(0);
                 });
+                low = kLowest;
                 if (edge(b + 1, there1)) mask(b + 1, there1, zn);
                 static_for<NW>([&](auto w) { power(w, z); });
                 static_for<NP>([&](auto n_) {
@@ -571,6 +573,7 @@ __global__ __launch_bounds__(kWave * P, DP > 128 ? 1 : 2) void attend_tile_kerne
                     score(n, zn);
                     __builtin_amdgcn_sched_barrier(0);
                 });
+                low = kLowest;
                 if (edge(b, there1)) mask(b, there1, zn);
                 static_for<NW>([&](auto w) { largest(w, zn); });
                 raise();
@@ -652,7 +655,7 @@ __global__ __launch_bounds__(kWave * P, DP > 128 ? 1 : 2) void attend_tile_kerne
                 l = __builtin_bit_cast(float, (uint32_t)s32[0]) + __builtin_bit_cast(float, (uint32_t)s32[1]);
                 if (xl >= wrows) {
                 } else if (w0 == w1) {
-                    const float inv = l > 0.0f || l != l ? 1.0f / l : 0.0f;  // no key: zeros
+                    const float inv = one_over(l, m);
                     T *yr = Y + (int64_t)(sv.q0 + tok) * a.ldy + (int64_t)(hk * g + r - tok * g) * a.d;
 #pragma unroll
                     for (int i = 0; i < ND; ++i)
@@ -715,7 +718,7 @@ __global__ __launch_bounds__(kWave * P, DP > 128 ? 1 : 2) void attend_tile_kerne
                         weight[w * kTileRows + r] = f;
                         all = __builtin_fmaf(f, sums[w * kTileRows + r], all);
                     }
-                    const float inv = all > 0.0f || all != all ? 1.0f / all : 0.0f;
+                    const float inv = one_over(all, top);
                     for (int w = 0; w < parts; ++w) weight[w * kTileRows + r] *= inv;
                 }
                 __syncthreads();
