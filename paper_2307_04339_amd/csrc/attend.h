@@ -60,6 +60,11 @@ __device__ __forceinline__ int64_t key_place(const AttendArgs &a, int64_t s, con
 
 __device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
 
+// Factors of partial results are at least the smallest number, so that an infinity among them stays one (0 times
+// infinity is none) however much smaller than the others' their maximum is.
+constexpr float kLeast = 0x1p-149f;
+__device__ __forceinline__ float part_factor(float m, float top) { return fmaxf(exp2_(m - top), kLeast); }
+
 // What a row's sums are multiplied by at last, m being its maximum.
 __device__ __forceinline__ float one_over(float l, float m) { return m == -INFINITY ? 0.0f : 1.0f / l; }
 
@@ -120,6 +125,33 @@ template <class T>
 __device__ __forceinline__ float not_finite_of(uint32_t w, int hi, bool seen) {
     constexpr uint32_t M = __is_same(T, half_t) ? 0x7c00u : 0x7f80u;
     return seen && ((hi ? w >> 16 : w) & M) == M ? unpack<T>(w, hi) : 0.0f;
+}
+
+// Whether the row at `pos` sees key j of its sequence.
+__device__ __forceinline__ bool sees(const AttendArgs &a, int pos, int j) {
+    return (!a.causal || j <= pos) && (a.window <= 0 || j > pos - a.window);
+}
+// And where every row sees such a value?  An infinity makes its output one however small its probability, but in
+// the products it may have met a 0, or the two numbers of a probability, which may differ in sign.  Outputs that are not
+// finite are therefore made once more, of such values alone: add(key, its offset in the cache) for each key of
+// [j0, j1) that is there, j0 >= 0.  Rare, so nothing is done for speed but to pass over absent pages.
+template <class F>
+__device__ __forceinline__ void each_key(const AttendArgs &a, int s, int j0, int j1, F &&add) {
+#pragma unroll 1
+    for (int j = j0; j < j1; ++j) {
+        const int64_t o = cache_place(a.sq, s, j);
+        if (o >= 0) add(j, o);
+        else j = ((int)fdiv((uint32_t)j, a.sq.fd_page) + 1) * a.sq.page - 1;
+    }
+}
+// Whether any of the values is an infinity or a NaN.
+template <int N, class V>
+__device__ __forceinline__ bool has_not_finite(const V &v) {
+    f32x4 t = {0.0f, 0.0f, 0.0f, 0.0f};  // 0 times such a value is NaN
+#pragma unroll
+    for (int i = 0; i < N; ++i) t[i % 4] = __builtin_fmaf(v[i], 0.0f, t[i % 4]);
+    const float s = (t[0] + t[1]) + (t[2] + t[3]);
+    return s != s;
 }
 
 // Cache policy of a buffer access with agent-scope coherence.

@@ -161,7 +161,7 @@ __global__ __launch_bounds__(kWave * P, DP > 128 ? 1 : 2) void attend_rows_kerne
                 float top = m;
 #pragma unroll
                 for (int q = 0; q < kJoin; ++q) top = fmaxf(top, mw[q]);
-                const float ms = top == -INFINITY ? 0.0f : top, f0 = exp2_(m - ms);
+                const float ms = top == -INFINITY ? 0.0f : top, f0 = part_factor(m, ms);
                 m = top;
                 l *= f0;
 #pragma unroll
@@ -169,7 +169,7 @@ __global__ __launch_bounds__(kWave * P, DP > 128 ? 1 : 2) void attend_rows_kerne
 #pragma unroll
                 for (int q = 0; q < kJoin; ++q) {
                     if (w + q >= n) continue;
-                    const float f = exp2_(mw[q] - ms);
+                    const float f = part_factor(mw[q], ms);
                     l = __builtin_fmaf(f, lw[q], l);
 #pragma unroll
                     for (int e = 0; e < 4; ++e) o[e] = __builtin_fmaf(f, ow[q][e], o[e]);
@@ -310,7 +310,6 @@ __global__ __launch_bounds__(kWave * P, DP > 128 ? 1 : 2) void attend_rows_kerne
                     const auto s32 = __builtin_amdgcn_permlane32_swap(w, w, false, false);
                     top = fmaxf(__builtin_bit_cast(float, (uint32_t)s32[0]), __builtin_bit_cast(float, (uint32_t)s32[1]));
                 }
-                if (row_seen) top = fmaxf(top, kLowest);
                 const float m1 = fmaxf(m, top), ms = m1 == -INFINITY ? 0.0f : m1;
                 const float alpha = m == -INFINITY ? 1.0f : exp2_(m - ms);  // (nothing to lower before the first key)
                 m = m1;
@@ -387,6 +386,20 @@ __global__ __launch_bounds__(kWave * P, DP > 128 ? 1 : 2) void attend_rows_kerne
                 l = __builtin_fmaf(f, part_l[w * 16 + r], l);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) o[e] = __builtin_fmaf(f, ow[e], o[e]);
+            }
+            // outputs that are not finite, and sums of 0 (no keys, or scores of -inf): see each_key
+            if (__builtin_expect(!(l > 0.0f) || has_not_finite<4>(o), 0)) {
+                const int pos = sv.pos0 + (int)fdiv((uint32_t)r, a.fd_group), j0 = (first + b0) * kRowKeys, j1 = (first + b1) * kRowKeys;
+                f32x4 only = {0.0f, 0.0f, 0.0f, 0.0f};
+                each_key(a, s, j0 > sv.begin ? j0 : sv.begin, j1 < sv.end ? j1 : sv.end, [&](int j, int64_t at) {
+                    if (!sees(a, pos, j)) return;
+                    m = fmaxf(m, kLowest);
+                    const u32x2 v = *reinterpret_cast<const u32x2 *>(vh + at + d4);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) only[e] += not_finite_of<T>(v[e >> 1], e & 1, true);
+                });
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[e] = only[e] == 0.0f ? o[e] : only[e];
             }
             if (whole) put(r, d4, o, m, l);
             else keep(slot0, r, d4, o, m, l);

@@ -648,6 +648,25 @@ __global__ __launch_bounds__(kWave * P, DP > 128 ? 1 : 2) void attend_tile_kerne
                     if (++b >= b1) break;
                 }
             }
+#pragma unroll
+            for (int i = 0; i < ND; ++i) {  // see each_key
+                if (__builtin_expect(__ballot(xl < wrows && has_not_finite<16>(acc[i])) == 0, 1)) continue;
+                acc_t only = {};
+                const int j0 = b0 * kTileKeys, j1 = b1 * kTileKeys;
+                each_key(a, s, j0 > tv.begin ? j0 : tv.begin, j1 < tv.end ? j1 : tv.end, [&](int j, int64_t o) {
+                    const bool in = sees(a, pos, j);
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        const int d = 32 * i + 8 * c + 4 * hx;
+                        if (d >= a.d) continue;
+                        const u32x2 w = *reinterpret_cast<const u32x2 *>(vh + o + d);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) only[4 * c + e] += not_finite_of<T>(w[e >> 1], e & 1, in);
+                    }
+                });
+#pragma unroll
+                for (int e = 0; e < 16; ++e) acc[i][e] = only[e] == 0.0f ? acc[i][e] : only[e];
+            }
             // ---- the rows' sums over both halves of the keys, then the output
             {
                 const uint32_t u = __builtin_bit_cast(uint32_t, l);
@@ -714,12 +733,12 @@ __global__ __launch_bounds__(kWave * P, DP > 128 ? 1 : 2) void attend_tile_kerne
                     for (int w = 0; w < parts; ++w) top = fmaxf(top, weight[w * kTileRows + r]);
                     const float ms = top == -INFINITY ? 0.0f : top;
                     for (int w = 0; w < parts; ++w) {
-                        const float f = exp2_(weight[w * kTileRows + r] - ms);
+                        const float f = part_factor(weight[w * kTileRows + r], ms);
                         weight[w * kTileRows + r] = f;
                         all = __builtin_fmaf(f, sums[w * kTileRows + r], all);
                     }
                     const float inv = one_over(all, top);
-                    for (int w = 0; w < parts; ++w) weight[w * kTileRows + r] *= inv;
+                    for (int w = 0; w < parts; ++w) weight[w * kTileRows + r] = fmaxf(weight[w * kTileRows + r] * inv, kLeast);
                 }
                 __syncthreads();
                 // piece i of a partial result: values 32 (i / 256 % ND) + 8 (i / 64 % 4) + 4 (i / 32 % 2) .. of row

@@ -96,3 +96,80 @@ def test_absent_pages_beside_scores_of_minus_infinity(ops, dtype, max_q):
     b.k[int(b.table[2, 3]), :, :, 0] = float("-inf")
     _, got = _run(ops, b, x, 2, 0, True, max_q)
     assert np.all(got[0] == 0) and np.all(np.isnan(got[1])) and np.all(np.isfinite(got[2])) and np.all(got[2] != 0)
+
+
+RISE = [
+    # new, ctx, heads, kv_heads, max_q, first key of the other level
+    ([1, 1], [400, 200], 2, 1, 1, 130),
+    ([1, 1], [9000, 5000], 4, 2, 1, 4500),           # divided among tiles
+    ([3], [300], 2, 2, 4, 140),
+    ([40, 1], [400, 200], 2, 1, None, 130),
+    ([33], [9000], 2, 1, None, 4500),                # divided among tiles
+]
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("levels", [(-10.0, 10.0), (10.0, -10.0), (0.0, 0.0), None])
+@pytest.mark.parametrize("case", RISE)
+def test_infinities_among_the_values_stay(ops, seq, dtype, levels, case):
+    """Values of +-inf at keys whose scores are 160 (231 powers of two) below those of later keys, or of earlier ones, or
+    as all others, or of any size: their weights are positive however small, so the outputs are +-inf."""
+    new, ctx, heads, kv, max_q, before = case
+    b = Batch(new, ctx, PAGE, kv, D, dtype, 320, behind=0).hide_unused()
+    x, x64 = rand((b.tokens, heads * D), dtype, 321, -2, 2)
+    if levels:                                       # 64 products of it, times 1 / 8
+        x, x64 = torch.ones_like(x), np.ones_like(x64)
+    plus, minus = 3, 40
+    for s, n in enumerate(ctx):
+        for j in range(n):
+            p, i = int(b.table[s, j // PAGE]), j % PAGE
+            if levels:
+                b.k64[p, :, i] = levels[j >= before]
+        late = levels and levels[1] < levels[0]
+        for j, c, v in [(n - new[s] - 6, plus, np.inf), (n - new[s] - 3, minus, -np.inf)] if late else [(2, plus, np.inf), (7, minus, -np.inf)]:
+            p, i = int(b.table[s, j // PAGE]), j % PAGE
+            b.v[p, :, i, c] = float(v)
+            b.v64[p, :, i, c] = v
+    b.k.copy_(torch.from_numpy(b.k64))
+    op, got = _run(ops, b, x, heads, 0, True, max_q)
+    assert max(ctx) < 1000 or op.info.ksplit > 1
+    h = seq.HALF_STEP[dtype]
+    want = seq.attention(x64, b.k64, b.v64, b.q_start, b.kv_len, b.table, heads, half_step=h, p_step=2 * h)
+    finite = [i for i in range(D) if i not in (plus, minus)]
+    for r, (w, e) in want.items():
+        g, w, e = (a.reshape(heads, D) for a in (got[r], w, e))
+        assert np.all(np.isposinf(w[:, plus])) and np.all(np.isneginf(w[:, minus]))
+        assert np.all(np.isposinf(g[:, plus])) and np.all(np.isneginf(g[:, minus])), r
+        assert np.all(np.abs(g[:, finite] - w[:, finite]) <= e[:, finite]), r
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("d,page,max_q", [(64, 16, 1), (80, 3, 1), (136, 16, 1), (64, 16, None), (80, 24, None), (96, 3, None), (128, 16, None), (200, 16, None)])
+def test_infinities_and_nan_of_both_signs(ops, seq, dtype, d, page, max_q):
+    """Every head size and page of both kernels, values of inf, -inf, both and NaN in columns of their own."""
+    b = Batch([1] if max_q else [45], [170], page, 2, d, dtype, 330, behind=0).hide_unused()
+    x, x64 = rand((b.tokens, 4 * d), dtype, 331, -2, 2)
+    cols = {0: [(4, np.inf)], 5: [(90, -np.inf)], d - 1: [(11, np.inf), (60, -np.inf)], d - 8: [(33, np.nan)], d // 2: [(50, np.inf), (51, np.inf)]}
+    for c, marks in cols.items():
+        for j, v in marks:
+            p, i = int(b.table[0, j // page]), j % page
+            b.v[p, :, i, c] = float(v)
+            b.v64[p, :, i, c] = v
+    y = sentinel((b.tokens, 4 * d), dtype)
+    q_start, kv_len, table = b.arrays()
+    op = ops.attention(x, b.k, b.v, y, q_start, kv_len, table, heads=4, max_q=max_q)
+    h = seq.HALF_STEP[dtype]
+    with np.errstate(invalid="ignore"):
+        want = seq.attention(x64, b.k64, b.v64, b.q_start, b.kv_len, b.table, 4, half_step=h, p_step=2 * h)
+    for block in (256, 128, 64):
+        y.fill_(-77.0)
+        op.launch(0, op.T, op.T, block)
+        torch.cuda.synchronize()
+        got = to_f64(y)
+        for r, (w, e) in want.items():
+            g, w, e = (a.reshape(4, d) for a in (got[r], w, e))
+            for c in range(d):
+                if c in cols:
+                    assert np.array_equal(g[:, c], w[:, c], equal_nan=True) and not np.any(np.isfinite(w[:, c])), (block, r, c)
+                else:
+                    assert np.all(np.abs(g[:, c] - w[:, c]) <= e[:, c]), (block, r, c)
