@@ -292,7 +292,7 @@ typedef enum {
      *   y = h;  z = N(h; pre, pre_bias), h as it is before its rounding to y.
      * N is RMS norm, v / sqrt(mean(v^2) + eps) * weight (+ bias), or layer norm (MIRIAM_SEQ_LAYER_NORM),
      * which subtracts the mean first.  residual, post, gate, the biases and either of y and z (with pre) may
-     * be absent.  Sums are held in fp32. */
+     * be absent.  Sums are held in fp32; a row whose sums leave its range is summed at a smaller scale. */
     MIRIAM_OP_BLOCK_NORM = 16,
     /* Rotary positions and the append to the cache.  x holds (heads + 2 kv_heads) heads of head_dim per row:
      * queries, keys, values.  Of the queries and keys the first `rot` values are turned pairwise by position *

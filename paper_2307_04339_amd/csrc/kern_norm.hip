@@ -84,17 +84,35 @@ __device__ __forceinline__ void norm_join(const NormArgs &a, float (&u)[N], int6
 #pragma unroll
     for (int e = 0; e < N; ++e) u[e] = a.res ? __builtin_fmaf(a.scale, u[e], r.at(e)) : a.scale * u[e];
 }
+// s and the values, c times as large; the squares of c (v - mean), cmean being c mean.
 template <int N>
-__device__ __forceinline__ float norm_add(float s, const float (&v)[N]) {
+__device__ __forceinline__ float norm_add(float s, const float (&v)[N], float c) {
 #pragma unroll
-    for (int e = 0; e < N; ++e) s += v[e];
+    for (int e = 0; e < N; ++e) s += v[e] * c;
     return s;
 }
 template <int N>
-__device__ __forceinline__ float norm_square(float s, const float (&v)[N], float mean) {
+__device__ __forceinline__ float norm_square(float s, const float (&v)[N], float c, float cmean) {
 #pragma unroll
-    for (int e = 0; e < N; ++e) s = __builtin_fmaf(v[e] - mean, v[e] - mean, s);
+    for (int e = 0; e < N; ++e) {
+        const float d = __builtin_fmaf(v[e], c, -cmean);
+        s = __builtin_fmaf(d, d, s);
+    }
     return s;
+}
+// Mean and 1 / sqrt(variance + eps) of a row.  sums(c, cmean) sets the mean of c v and returns that of (c (v - mean))^2.
+// A row whose sums leave fp32 is summed once more, its values 2^-80 as large: the largest ones' squares are 2^96 then, and
+// what vanishes beside those that left it is below 2^-46.
+template <class F>
+__device__ __forceinline__ void norm_stats(const NormArgs &a, F &&sums, float &mean, float &rstd) {
+    constexpr float kSmall = 0x1p-80f;
+    const float var = sums(1.0f, mean);
+    rstd = 1.0f / sqrtf(var + a.eps);
+    if (__builtin_expect(!(var < INFINITY), 0)) {
+        const float small = sums(kSmall, mean);
+        mean *= 1.0f / kSmall;
+        rstd = kSmall / sqrtf(small + a.eps * kSmall * kSmall);
+    }
 }
 
 // WR: logical waves per row; NR: vectors of V values per lane that are kept (0: the row is read again for each
@@ -114,9 +132,8 @@ __global__ __launch_bounds__(kWave * P) void norm_kernel(NormArgs a, Shard sh) {
     const float inv_n = 1.0f / (float)a.n;
     const int64_t whole = RAG ? a.n / V * V : a.n;  // the rest: one element of the row's first lanes
     const bool rows_gate = a.gate_kind > GATE_CHANNEL;
-    // mean over the row from its lanes' sums (divided by n first: the row's sum of squares may be beyond fp32
-    // where their mean is not), in LDS over its four logical waves: two places in turn, as a wave is at most one
-    // meeting ahead of another's reads
+    // mean over the row from its lanes' sums (divided by n first), in LDS over its four logical waves: two places in
+    // turn, as a wave is at most one meeting ahead of another's reads
     int turn = 0;
     auto row_mean = [&](const float (&part)[SL]) {
         if constexpr (WR == 1) {
@@ -186,22 +203,22 @@ __global__ __launch_bounds__(kWave * P) void norm_kernel(NormArgs a, Shard sh) {
                         for (int e = 0; e < V; ++e) v[i][e] = x[i].at(e);
                     });
                 }
-                auto stats = [&](float &mean, float &rstd) {
+                auto sums = [&](float c, float &cmean) __attribute__((always_inline)) {
                     float part[1] = {0.0f};
-                    mean = 0.0f;
+                    cmean = 0.0f;
                     if (a.layer) {
-                        each([&](int i, int64_t) { part[0] = norm_add(part[0], v[i]); });
-                        if (rest) part[0] = norm_add(part[0], vt);
-                        mean = row_mean(part);
+                        each([&](int i, int64_t) { part[0] = norm_add(part[0], v[i], c); });
+                        if (rest) part[0] = norm_add(part[0], vt, c);
+                        cmean = row_mean(part);
                         part[0] = 0.0f;
                     }
-                    each([&](int i, int64_t) { part[0] = norm_square(part[0], v[i], mean); });
-                    if (rest) part[0] = norm_square(part[0], vt, mean);
-                    rstd = 1.0f / sqrtf(row_mean(part) + a.eps);
+                    each([&](int i, int64_t) { part[0] = norm_square(part[0], v[i], c, cmean); });
+                    if (rest) part[0] = norm_square(part[0], vt, c, cmean);
+                    return row_mean(part);
                 };
                 float mean, rstd;
                 if (a.post) {
-                    stats(mean, rstd);
+                    norm_stats(a, sums, mean, rstd);
                     each([&](int i, int64_t j) { norm_apply<V, RAG>(v[i], j, a.post, a.post_bias, mean, rstd); });
                     if (rest) norm_apply<1, RAG>(vt, jt, a.post, a.post_bias, mean, rstd);
                 }
@@ -214,7 +231,7 @@ __global__ __launch_bounds__(kWave * P) void norm_kernel(NormArgs a, Shard sh) {
                     if (a.y) put_row<T, 1, RAG>(yr + jt, vt, a.past);
                 }
                 if (a.z) {
-                    stats(mean, rstd);
+                    norm_stats(a, sums, mean, rstd);
                     each([&](int i, int64_t j) {
                         norm_apply<V, RAG>(v[i], j, a.pre, a.pre_bias, mean, rstd);
                         put_row<T, V, RAG>(zr + j, v[i], a.past);
@@ -243,9 +260,9 @@ __global__ __launch_bounds__(kWave * P) void norm_kernel(NormArgs a, Shard sh) {
                     if (a.post) norm_apply<N, RAG>(v, j, a.post, a.post_bias, m1, r1);
                     norm_join<N, RAG>(a, v, j, r, g);
                 };
-                auto stats = [&](auto &&get, float &mean, float &rstd) {
-                    float part[SL] = {};
-                    mean = 0.0f;
+                auto sums = [&](auto &&get, float c, float &cmean) __attribute__((always_inline)) {
+                    float part[SL] = {}, total = 0.0f;
+                    cmean = 0.0f;
                     float v[V], vt[1];
                     for (int pass = a.layer ? 0 : 1; pass < 2; ++pass) {
 #pragma unroll
@@ -253,17 +270,20 @@ __global__ __launch_bounds__(kWave * P) void norm_kernel(NormArgs a, Shard sh) {
                             part[s] = 0.0f;
                             for (int64_t j = col0(s); j < whole; j += step) {
                                 get(v, j);
-                                part[s] = pass == 0 ? norm_add(part[s], v) : norm_square(part[s], v, mean);
+                                part[s] = pass == 0 ? norm_add(part[s], v, c) : norm_square(part[s], v, c, cmean);
                             }
                             if (rest && s == 0) {
                                 get(vt, jt);
-                                part[s] = pass == 0 ? norm_add(part[s], vt) : norm_square(part[s], vt, mean);
+                                part[s] = pass == 0 ? norm_add(part[s], vt, c) : norm_square(part[s], vt, c, cmean);
                             }
                         }
-                        const float total = row_mean(part);
-                        if (pass == 0) mean = total;
-                        else rstd = 1.0f / sqrtf(total + a.eps);
+                        total = row_mean(part);
+                        if (pass == 0) cmean = total;
                     }
+                    return total;
+                };
+                auto stats = [&](auto &&get, float &mean, float &rstd) {
+                    norm_stats(a, [&](float c, float &cmean) { return sums(get, c, cmean); }, mean, rstd);
                 };
                 if (a.post) stats(load, m1, r1);
                 if (a.z) stats(joined, m2, r2);
