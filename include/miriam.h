@@ -304,18 +304,19 @@ typedef enum {
     MIRIAM_OP_ROTARY = 17,
     /* Attention of the new tokens over the paged cache: y = sum_j softmax_j(scale * q . k_j) v_j for every
      * query head, heads / kv_heads consecutive ones sharing a cache head, over the keys j < kv_len[s] that
-     * are there and, with MIRIAM_SEQ_CAUSAL, at or before the token's position, and with window > 0 among the
-     * `window` last ones up to it.  A row without keys gives zeros, one that sees keys whose scores are all -inf
-     * NaN; an infinity among the values that a row sees makes its output one, however small its probability (NaN
-     * beside one of the other sign); and what a row does not see never reaches it, whatever it holds (infinities
-     * and NaN included).  fp16 / bf16, head_dim a multiple of 8 up to 256, scale > 0; x, y and the caches 16-byte
-     * aligned, their strides multiples of 8.  max_q: most new tokens of one sequence (0 = tokens); rows of a
-     * sequence behind its max_q-th are left as they were.  Up to 16 query rows per cache head (max_q * heads /
-     * kv_heads) have a kernel of their own; beyond, page * max_pages must be below 2^26, and probabilities are
-     * rounded to the operator's type before they meet the values.  Keys may be divided among tiles, whose partial
-     * results the last one to finish joins in a fixed order: such an op (miriam_op_info.ksplit = 2) owns a device
-     * workspace (for many rows up to 69 MB at a head_dim of 128) and arrival counters, with the rules of split K:
-     * every pass covers the whole tile space, passes over one op do not overlap in time. */
+     * are there, with MIRIAM_SEQ_CAUSAL at or before the token's position p, and with window > 0 after p - window
+     * (the last `window` ones up to its own, and without MIRIAM_SEQ_CAUSAL all later ones).  A row without keys
+     * gives zeros, one that sees keys whose scores are all -inf NaN; an infinity among the values that a row sees
+     * makes its output one, however small its probability (NaN beside one of the other sign); and what a row does
+     * not see never reaches it, whatever it holds (infinities and NaN included).  fp16 / bf16, head_dim a multiple
+     * of 8 up to 256, scale > 0; x, y and the caches 16-byte aligned, their strides multiples of 8.  max_q: most
+     * new tokens of one sequence (0 = tokens); rows of a sequence behind its max_q-th are left as they were.  Up
+     * to 16 query rows per cache head (max_q * heads / kv_heads) have a kernel of their own; beyond, page *
+     * max_pages must be below 2^26, and probabilities are rounded to the operator's type before they meet the
+     * values.  Keys may be divided among tiles, whose partial results the last one to finish joins in a fixed
+     * order: such an op (miriam_op_info.ksplit = 2) owns a device workspace (for many rows up to 69 MB at a
+     * head_dim of 128) and arrival counters, with the rules of split K: every pass covers the whole tile space,
+     * passes over one op do not overlap in time. */
     MIRIAM_OP_ATTENTION = 18
 } miriam_seq_kind;
 

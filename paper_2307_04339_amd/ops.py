@@ -315,8 +315,8 @@ def rotary(x, y, freq, q_start, kv_len, *, heads, head_dim, kv_heads=0, k_cache=
 
 def attention(q, k_cache, v_cache, y, q_start, kv_len, page_table, *, heads, scale=None, causal=True, window=0, max_q=None):
     """y = attention of the new tokens' queries q [tokens, heads * head_dim] over their sequences' cached keys
-    (those of the new tokens among them).  scale: 1 / sqrt(head_dim) if None.  window > 0: only the last `window`
-    keys up to a token's own.  max_q: most new tokens of one sequence (all rows if None); knowing that it is
+    (those of the new tokens among them).  scale: 1 / sqrt(head_dim) if None.  window > 0: of the keys up to
+    a token's own only the last `window` (without causal all later ones, too).  max_q: most new tokens of one sequence (all rows if None); knowing that it is
     small gives the kernel for single tokens.  The arrays of a batch must not change during a pass."""
     _one_device(q=q, k_cache=k_cache, v_cache=v_cache, y=y, q_start=q_start, kv_len=kv_len, page_table=page_table)
     f = _sequences(q_start, kv_len, page_table, k_cache, v_cache, q.dtype)

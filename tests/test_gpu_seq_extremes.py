@@ -173,3 +173,21 @@ def test_infinities_and_nan_of_both_signs(ops, seq, dtype, d, page, max_q):
                     assert np.array_equal(g[:, c], w[:, c], equal_nan=True) and not np.any(np.isfinite(w[:, c])), (block, r, c)
                 else:
                     assert np.all(np.abs(g[:, c] - w[:, c]) <= e[:, c]), (block, r, c)
+
+
+@pytest.mark.parametrize("new,max_q", [(4, 4), (50, None)])
+@pytest.mark.parametrize("causal,window", [(True, 0), (True, 7), (False, 0), (False, 7)])
+def test_what_a_window_shows(ops, new, max_q, causal, window):
+    """Values that say which key they belong to: a window hides the keys p - window and before, causal those after p."""
+    ctx = 60
+    b = Batch([new], [ctx], PAGE, 1, D, "f16", 340, behind=0)
+    b.k.zero_()                                      # every key of the same weight
+    for j in range(ctx):
+        b.v[int(b.table[0, j // PAGE]), 0, j % PAGE] = 0.0
+        b.v[int(b.table[0, j // PAGE]), 0, j % PAGE, j] = 1.0
+    x, _ = rand((new, D), "f16", 341)
+    _, got = _run(ops, b, x, 1, window, causal, max_q)
+    for r in range(new):
+        p = ctx - new + r
+        shown = {j for j in range(ctx) if (not causal or j <= p) and (not window or j > p - window)}
+        assert set(np.flatnonzero(got[r])) == shown, r
