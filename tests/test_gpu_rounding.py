@@ -29,3 +29,24 @@ def test_resident_conv_with_affine_epilogue_in_every_block(dtype, n, hw, c, k):
         torch.cuda.synchronize()
         got.append(bits(y))
     assert got[0] == got[1] == got[2]
+
+
+@pytest.mark.parametrize("act", ["relu", "relu6", "gelu"])
+def test_resident_conv_with_an_activation_in_every_block(act):
+    from paper_2307_04339_amd import _lib as L
+    from paper_2307_04339_amd import ops
+    n, hw, c, k = 16, 56, 64, 64
+    x, _ = rand((n, hw, hw, c), "f16", 44)
+    w, _ = rand((k, 3, 3, c), "f16", 45, -0.2, 0.2)
+    rng = np.random.default_rng(46)
+    bn = f32_dev(np.stack([rng.uniform(0.8, 1.2, k), rng.uniform(-0.1, 0.1, k), rng.uniform(-0.1, 0.1, k), rng.uniform(0.8, 1.2, k)]))
+    y = empty((n, hw, hw, k), "f16")
+    op = ops.conv2d(x, w, y, stride=1, pad=1, bias=None, bn=bn, residual=None, act=act, tile=8)
+    assert op.info.path == L.PATH_RESIDENT
+    got = []
+    for block in (64, 128, 256):
+        y.fill_(float("nan"))
+        op.launch(0, op.T, op.T, block)
+        torch.cuda.synchronize()
+        got.append(bits(y))
+    assert got[0] == got[1] == got[2]
