@@ -15,7 +15,8 @@
 //
 // Measured: 48 sequences of 200 to 8000 keys, 32 heads over 8 cache heads of 128: 105 us, 4.8 TB/s (a copy 4.9); two
 // of 100k to 131k keys, 16 heads over 2: 57 us, 4.0 TB/s, of which some 10 to find the work and to join 256 partial
-// results per head in two stages; one token behind 128 keys 8 us, where a launch takes 4.
+// results per head in two stages; one token behind 128 keys 7.5 us, where a launch takes 4 and each of 12 of the 256 CUs
+// then reads lengths, page, keys and values one after the other, for two blocks.
 //
 // P is the sum of two 16-bit numbers (its rounding and the rest), which keeps the output at the
 // rounding of its own type and costs matrix instructions that wait for memory anyway.
@@ -84,7 +85,7 @@ __global__ __launch_bounds__(kWave * P, DP > 128 ? 1 : 2) void attend_rows_kerne
     // longer than one, and most heads of short sequences need no joining.
     int total = 0, share = 0, ahead = 0;  // ahead: places up to and with the lane's part of the sequences
     bool even = false;
-    const int per = (seqs + kWave - 1) / kWave;  // sequences of a lane's part (300 of 300 keys, one cache head: 40 us, 64 after 64: 61)
+    const int per = (seqs + kWave - 1) / kWave;  // sequences of a lane's part (300 of 300 keys, one cache head: 41 us, 64 after 64: 61)
     if (a.splits > 1) {
         int sum = 0, pairs = 0;
         if (per == 1) {

@@ -25,14 +25,17 @@
 // A row tile that ends up in several tiles is joined by the last of them to arrive, in their order.
 //
 // Probabilities are rounded once, to T, as the matrix instructions take them, and the sum that divides the output is
-// that of the rounded ones (fp32), so a row's weights still add up to one.  The two numbers per probability of the
-// kernel for few rows would cost half of the products again here, where these bound it.
+// that of the rounded ones (fp32), so a row's weights still add up to one.  Each weight is then off by half a step of T at
+// most, and an output of values of both signs by about as much as its own rounding: against 64 bits 0.0024 of its size
+// in bf16 and 0.00026 in fp16, where rounding the output alone gives 0.0017 and 0.00020.  The two numbers per probability
+// of the kernel for few rows give that here, too, but take half of the products again where these bound it: whole
+// prompts 679 -> 858 us, a chunk behind 16k 174 -> 220, the 20 sequences 55 -> 62.
 //
 // Measured, with that division and loads whose addresses the lanes work out: 4 prompts of 4096 tokens, 32 heads of
-// 128: 640 us, 860 TFLOP/s of the products that are needed (a wave's vector and matrix instructions together keep a
-// SIMD busy for 85% of that, and neither their order nor their waves' priorities matter: the clock falls under
-// them); a chunk of 512 tokens behind 16k 161 us; the 20 sequences (heads of 80) 53 us, of which 5 to find the work, 8 for
-// starts and outputs of row tiles and 11 for joining.
+// 128: 640 to 720 us by box and its clock, 760 to 860 TFLOP/s of the products that are needed (a wave's vector and
+// matrix instructions together keep a SIMD busy for 85% of that, and neither their order nor their waves' priorities
+// matter: the clock falls under them); a chunk of 512 tokens behind 16k 162 to 175 us; the 20 sequences (heads of 80)
+// 53 us, of which 5 to find the work, 8 for starts and outputs of row tiles and 11 for joining.
 #pragma once
 
 #include "attend.h"
@@ -129,7 +132,7 @@ __global__ __launch_bounds__(kWave * P, DP > 128 ? 1 : 2) void attend_tile_kerne
     };
     // row tiles of a cache head, the longest sequence's steps, and at least half of all; a lane goes through its part
     // of the sequences, so that a tile need not look through all of them again (1000 sequences of 128 tokens, 12
-    // heads of 64: 430 us, 64 sequences after 64 twice 581)
+    // heads of 64: 438 us, 64 sequences after 64 twice 581)
     const int per = (seqs + kWave - 1) / kWave;
     int J = 0, longest = 0;
     float half = 0.0f;

@@ -6,8 +6,8 @@
 // itself would be off by 0.06 radians there).  What is left, an eighth of a turn at most beside a multiple of a
 // quarter, goes into the power series of sine and cosine, cut where the next term is below 2^-25.
 //
-// What bounds it: HBM, every value read and written once (8192 tokens of 48 heads of 128 bf16: 41 us, 4.9 TB/s, as a
-// copy; 128 tokens: 5 us, hardly more than a launch).  A lane keeps its place in the head over all heads of
+// What bounds it: HBM, every value read and written once (8192 tokens of 48 heads of 128 bf16: 40 us, 5.1 TB/s past the
+// caches, where a plain copy reaches 4.9; 128 tokens: 5 us, hardly more than a launch).  A lane keeps its place in the head over all heads of
 // its token, so a row's angles are computed once per wave; loads of four rounds over the heads are in flight
 // at once.  Few tokens: a row's heads are divided among several waves (RotaryArgs::parts).
 #include "seq_rows.h"

@@ -8,9 +8,9 @@ namespace miriam {
 // Ops that move more than this read and write their rows past the caches: nothing would be left in L2 (8 x 4 MB) for
 // a reader anyway, and lines that are used once no longer take places from others; and their tiles go over the dies
 // in turn, so that all memory channels are busy at once.  With buffers that the last-level cache does not hold: norms
-// of 8192 rows of 4096 69 -> 57 us (outputs alone 63, tiles in turn 60), positions of 8192 tokens of 48 heads of
-// 128 49 -> 41 us (47, 45).  Norms and then a reader of both outputs, of buffers that it does hold: 134 MB 50.4 ->
-// 49.2 us, 67 MB 27.7 -> 28.9, 34 MB 21.4 -> 19.8.
+// of 8192 rows of 4096 69 -> 53 us (outputs alone 63, tiles in turn 60), positions of 8192 tokens of 48 heads of
+// 128 49 -> 40 us (47, 45).  Where it does hold them, the limit matters little either way: norms and then a reader of both
+// outputs 50.4 -> 49.2 us at 134 MB, 27.7 -> 28.9 at 67 MB, 21.4 -> 19.8 at 34 MB.
 constexpr double kPastBytes = 32e6;
 
 // The norms around a block.
