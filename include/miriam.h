@@ -283,8 +283,8 @@ int miriam_op_destroy(miriam_op *op);
  * The coordinator runs an operator several times when it measures it, so none of these works in place: an
  * output (for ROTARY the caches, too) that overlaps rows, weights, caches, frequencies or the batch's arrays that
  * are read is refused (columns of their own in rows of one buffer are no overlap).  ROTARY wants two caches all of
- * whose places are their own: they may be interleaved, but of pages, heads, tokens and the two caches each must
- * step past all that the ones of shorter steps reach.
+ * whose places are their own: of pages, heads and tokens each must step past all that the ones of shorter steps
+ * reach, and the two may be interleaved but share none.
  */
 typedef enum {
     /* Norms around a block, with its gate and residual, over rows of n values:

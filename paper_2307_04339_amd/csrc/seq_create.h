@@ -75,21 +75,42 @@ static bool over_batch(const miriam_seq_desc &d, const SeqArgs &q, const Rows &o
            overlap({q.table, q.seqs, d.max_pages, q.ldt, 4}, out);
 }
 
-// Whether all places of two caches of the same strides, `apart` elements from one to the other, are of their own: of
-// the dimensions with more than one entry, the caches themselves among them, each must step past all that the ones of
-// shorter steps reach.  (So caches may lie one behind the other, or interleaved at any level.)
-static bool own_places(const miriam_seq_desc &d, int64_t apart) {
-    struct Dim {
+// Dimensions of a cache, by their steps (those of one entry, which step nowhere, first).
+struct CacheDims {
+    struct {
         int64_t step, n;
-    } dims[4] = {{d.cache_page, d.pages}, {d.cache_head, d.kv_heads}, {d.cache_token, d.page}, {apart, 2}};
-    std::sort(dims, dims + 4, [](const Dim &a, const Dim &b) { return a.step < b.step; });
-    int64_t reach = d.head_dim;
-    for (const Dim &m : dims) {
+    } dim[3];
+};
+static CacheDims cache_dims(const miriam_seq_desc &d) {
+    CacheDims c = {{{d.cache_page, d.pages}, {d.cache_head, d.kv_heads}, {d.cache_token, d.page}}};
+    for (auto &m : c.dim)
+        if (m.n < 2) m.step = 0;
+    std::sort(c.dim, c.dim + 3, [](const auto &a, const auto &b) { return a.step < b.step; });
+    return c;
+}
+
+// Whether each dimension steps past all that the ones of shorter steps reach: every place of the cache is its own then.
+static bool own_places(const CacheDims &c, int64_t head_dim) {
+    int64_t reach = head_dim;
+    for (const auto &m : c.dim) {
         if (m.n < 2) continue;
         if (m.step < reach) return false;
         reach += (m.n - 1) * m.step;
     }
     return true;
+}
+
+// Whether two such caches, `apart` values from one to the other, share a place: whether apart is a sum of steps and of
+// less than a head.  What is left for the shorter steps is less than the longest one, so only the two multiples of that
+// next to `apart` may be among them.
+static bool share_places(const CacheDims &c, int64_t head_dim, int64_t apart, int dims = 3) {
+    if (dims == 0) return apart < head_dim && -apart < head_dim;
+    const auto &m = c.dim[dims - 1];
+    if (m.n < 2) return share_places(c, head_dim, apart, dims - 1);
+    const int64_t q = apart / m.step - (apart % m.step < 0 ? 1 : 0);  // floor
+    for (int64_t k = q; k <= q + 1; ++k)
+        if (k < m.n && -k < m.n && share_places(c, head_dim, apart - k * m.step, dims - 1)) return true;
+    return false;
 }
 
 // The heads of a descriptor.
@@ -192,8 +213,10 @@ static int create_rotary(miriam_op *op) {
         if (a.k == a.v) return einval("rotary: both caches are one");
         // (two stores to one place would leave either)
         const uintptr_t ka = (uintptr_t)a.k, va = (uintptr_t)a.v, bytes = ka < va ? va - ka : ka - va;
-        if (!own_places(d, (int64_t)std::min<uintptr_t>(bytes / (uintptr_t)es, (uintptr_t)1 << 62)))
-            return einval("rotary: places of the caches overlap (each stride must step past what the shorter ones reach)");
+        const CacheDims dims = cache_dims(d);
+        if (!own_places(dims, d.head_dim)) return einval("rotary: places of a cache overlap (each stride must step past what the shorter ones reach)");
+        if (share_places(dims, d.head_dim, (int64_t)std::min<uintptr_t>(bytes / (uintptr_t)es, (uintptr_t)1 << 62)))
+            return einval("rotary: places of the two caches overlap");
         if (overlap(x, k) || overlap(x, v) || overlap(y, k) || overlap(y, v)) return einval("rotary: x or y overlaps a cache");
         for (const Rows &c : {k, v})
             if (over_batch(d, a.sq, c) || overlap(freq, c)) return einval("rotary: a cache overlaps q_start, kv_len, page_table or freq");

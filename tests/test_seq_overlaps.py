@@ -32,6 +32,8 @@ def _accepted(L, base, changes):
     dict(cache_head=64, cache_token=64),
     dict(cache_page=1024, cache_head=2048),                          # pages within the heads' steps, but longer than theirs
     dict(v_cache=_at(3) + 64 * ES, cache_token=96, cache_head=1536, cache_page=3072),   # interleaved, tokens too near
+    dict(v_cache=_at(3) + (4096 * 3 + 2000) * ES, cache_page=4096),  # reaching into the pages it should lie between
+    dict(v_cache=_at(3) - 4096 * 7 * ES, cache_page=4096),           # its last page is k's first
 ])
 def test_caches_whose_places_overlap_are_refused(L, changes):  # noqa: F811
     assert b"overlap" in _refused(L, ROT, changes)
@@ -44,6 +46,8 @@ def test_caches_whose_places_overlap_are_refused(L, changes):  # noqa: F811
     dict(v_cache=_at(3) + 1024 * ES, cache_page=4096, cache_head=2048),                  # of a head
     dict(v_cache=_at(3) + 64 * ES, cache_token=128, cache_head=2048, cache_page=4096),   # of a token
     dict(v_cache=_at(3) + 128 * ES, cache_token=256, cache_head=64, cache_page=4096),    # of a token's heads
+    dict(v_cache=_at(3) + (4096 * 3 + 2048) * ES, cache_page=4096),  # keys and values in turn, some pages later
+    dict(v_cache=_at(3) - 4096 * 8 * ES, cache_page=4096),
     dict(cache_token=128, cache_head=64),                            # a token's heads together
     dict(cache_page=64, cache_token=512, cache_head=512 * 16),       # pages innermost
     dict(kv_heads=1, cache_head=1), dict(pages=1, cache_page=1),     # steps that nothing takes
@@ -53,24 +57,31 @@ def test_caches_of_their_own_places_are_accepted(L, changes):  # noqa: F811
 
 
 def test_what_is_accepted_has_places_of_its_own(L):  # noqa: F811
-    """Every accepted combination of small strides, place by place."""
+    """Small strides and distances, place by place: what is accepted has places of its own, dense caches of such places
+    are accepted, and beside a cache that is accepted any other that shares none."""
     pages, kv, page, d = 3, 2, 2, 2
     base = dict(ROT, pages=pages, kv_heads=kv, page=page, head_dim=d, rot=2, heads=2)
     grid = np.array(list(itertools.product(range(pages), range(kv), range(page))))
-    taken = 0
-    for sp, sh, st in itertools.product((2, 3, 4, 6, 8, 12), repeat=3):
-        for apart in (2, 4, 6, 8, 12, 24, 64):
-            rc, h = _create(L, **dict(base, cache_page=sp, cache_head=sh, cache_token=st, v_cache=_at(3) + apart * ES))
-            at = (grid @ np.array([sp, sh, st]))[:, None] + np.arange(d)
-            both = np.concatenate([at, at + apart]).ravel()
-            if rc == 0:
-                taken += 1
-                assert len(set(both)) == len(both), (sp, sh, st, apart)
-                L.load().miriam_op_destroy(h)
-            # (what a contiguous allocation gives is accepted)
-            elif len(set(both)) == len(both):
-                assert max(both) + 1 > len(both), (sp, sh, st, apart)
-    assert taken > 10
+
+    def accepted(**changes):
+        rc, h = _create(L, **dict(base, **changes))
+        if rc == 0:
+            L.load().miriam_op_destroy(h)
+        return rc == 0
+
+    pairs = interleaved = 0
+    for sp, sh, st in itertools.product((2, 3, 4, 6, 8, 12, 16, 24), repeat=3):
+        at = ((grid @ np.array([sp, sh, st]))[:, None] + np.arange(d)).ravel()
+        strides = dict(cache_page=sp, cache_head=sh, cache_token=st)
+        alone, own = accepted(**strides), len(set(at)) == len(at)       # (the other cache is far away)
+        assert own or not alone, strides
+        assert alone or not own or max(at) + 1 > len(at), strides
+        for apart in list(range(-40, 41)) if alone else ():
+            ok = accepted(**strides, v_cache=_at(3) + apart * ES)
+            assert ok == (not set(at) & set(at + apart)), (strides, apart)
+            pairs += ok
+            interleaved += ok and abs(apart) <= max(at)
+    assert pairs > 100 and interleaved > 100
 
 
 # --------------------------------------------- outputs over what a pass reads
