@@ -191,3 +191,16 @@ def test_what_a_window_shows(ops, new, max_q, causal, window):
         p = ctx - new + r
         shown = {j for j in range(ctx) if (not causal or j <= p) and (not window or j > p - window)}
         assert set(np.flatnonzero(got[r])) == shown, r
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("new,ctx,heads,kv,max_q", [([1], [1], 2, 1, 1), ([1, 1], [40, 9000], 4, 2, 1), ([3], [40], 2, 2, 4),
+                                                    ([20, 1], [20, 1], 2, 1, None), ([33], [9000], 2, 1, None)])
+def test_keys_that_are_all_nan(ops, dtype, new, ctx, heads, kv, max_q):
+    """Rows that see nothing but scores of NaN give NaN, rows without keys beside them zeros."""
+    b = Batch(new + [1], ctx + [0], PAGE, kv, D, dtype, 350, behind=1).hide_unused()
+    b.k.fill_(float("nan"))
+    x, _ = rand((b.tokens, heads * D), dtype, 351)
+    _, got = _run(ops, b, x, heads, 0, True, max_q)
+    n = sum(new)
+    assert np.all(np.isnan(got[:n])) and np.all(got[n] == 0) and np.all(got[n + 1] == -77.0)
