@@ -31,7 +31,7 @@ def _accepted(L, base, changes):
     dict(cache_head=8), dict(cache_page=64),                         # heads, pages that overlap
     dict(cache_head=64, cache_token=64),
     dict(cache_page=1024, cache_head=2048),                          # pages within the heads' steps, but longer than theirs
-    dict(v_cache=_at(3) + 64 * ES, cache_token=96, cache_head=1536, cache_page=3072),   # interleaved, tokens too near
+    dict(v_cache=_at(3) + 64 * ES, cache_token=96, cache_head=1600, cache_page=3200),   # interleaved, tokens too near
     dict(v_cache=_at(3) + (4096 * 3 + 2000) * ES, cache_page=4096),  # reaching into the pages it should lie between
     dict(v_cache=_at(3) - 4096 * 7 * ES, cache_page=4096),           # its last page is k's first
 ])
