@@ -34,7 +34,7 @@
 // Measured, with that division and loads whose addresses the lanes work out: 4 prompts of 4096 tokens, 32 heads of
 // 128: 640 to 720 us by box and its clock, 760 to 860 TFLOP/s of the products that are needed (a wave's vector and
 // matrix instructions together keep a SIMD busy for 85% of that, and neither their order nor their waves' priorities
-// matter: the clock falls under them); a chunk of 512 tokens behind 16k 162 to 175 us; the 20 sequences (heads of 80)
+// matter: the clock falls under them); a chunk of 512 tokens behind 16k 160 to 175 us; the 20 sequences (heads of 80)
 // 53 us, of which 5 to find the work, 8 for starts and outputs of row tiles and 11 for joining.
 #pragma once
 
